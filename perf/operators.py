@@ -5,8 +5,8 @@ kind      one pass
           loss and, with "grad", the gradient of the sum of those means for the hidden states (tlora_ce_fwd, tlora_ce_fwd_bwd)
 "norm"    residual stream and norms between two blocks: H = X + res_scale * gate_j * norm(Y; gamma_post), Xn = norm(H; gamma_pre)
           (tlora_norm_fwd), or with "grad" its gradient for the stream, the block's output, both gammas and the gates (tlora_norm_bwd)
-"act8"    an activation into 8 bits and back (tlora_act8_pack, tlora_act8_unpack)
-"bwd8"    the fused layer's backward whose X was kept in 8 bits (tlora_bwd_act8)
+"act8"    an activation into 8 bits and back (tlora_ckpt_pack, tlora_ckpt_unpack)
+"bwd8"    the fused layer's backward whose X was kept in 8 bits (tlora_bwd_ckpt)
 
 Lists of per-job numbers are texts ("8,16,32").  Hidden states and upstream gradients are N(0, 1), the vocabulary projection
 N(0, 1 / d_model) times 2 (logits of standard deviation 2), gammas and gates N(1, 0.1), adapters as in the benchmark's workloads.
@@ -176,7 +176,7 @@ def _prepare_bwd8(case, seed):
     st["A"] = [((x.uniform(d_in, r) * 2 - 1) / d_in ** 0.5).to(x.dtype) for r in ranks]
     st["B"] = [x.normal(r, d_out, std=0.01) for r in ranks]
     codes, scales = _quantise(st["X"])
-    # the packed form as tlora_act8_pack lays it out: all codes, then the scales from the next multiple of 256 bytes on
+    # the packed form as tlora_ckpt_pack lays it out: all codes, then the scales from the next multiple of 256 bytes on
     at = (codes.numel() + 255) // 256 * 256
     st["packed"] = torch.zeros((at + 2 * scales.numel() + 255) // 256 * 256, dtype=torch.uint8, device="cuda")
     st["packed"][:codes.numel()] = codes.reshape(-1).view(torch.uint8)
@@ -223,14 +223,14 @@ def _prepare_own(case, st):
             st["out"] = {"H": torch.empty_like(st["X"]), "Xn": torch.empty_like(st["X"])}
     elif kind == "act8":
         T, d = st["X"].shape
-        st["act8"] = tlora.Act8(case["dtype"], T, d, "cuda")
+        st["act8"] = tlora.Checkpoint(case["dtype"], T, d, "cuda")
         st["out"] = torch.empty_like(st["X"])
     else:
         d_in, d_out = _ints(case["dims"].replace("x", ","))
         st["layer"] = tlora.LayerProblem(case["dtype"], d_in, d_out, st["ranks"], st["offsets"], st["scales"], st["X"], st["W"],
                                          st["A"], st["B"])
         Y, dX, dA, dB = st["layer"].new_outputs()
-        st["layer"].bwd_act8_workspace()
+        st["layer"].bwd_ckpt_workspace()
         if case["reuse_S"]:
             st["layer"].fwd(Y)
         st["out"] = {"dX": dX if case["want_dX"] else None, "dA": dA, "dB": dB}
@@ -265,7 +265,7 @@ def _run_own(case, st):
         st["act8"].unpack(st["out"])
         return st["out"]
     out = st["out"]
-    st["layer"].bwd_act8(st["packed"], st["dY"], out["dX"], out["dA"], out["dB"], reuse_S=case["reuse_S"])
+    st["layer"].bwd_ckpt(st["packed"], st["dY"], out["dX"], out["dA"], out["dB"], reuse_S=case["reuse_S"])
     return {k: v for k, v in out.items() if v is not None}
 
 
