@@ -332,6 +332,93 @@ int tlora_layer_fwd(const tlora_layer_t* p, void* Out, void* workspace, size_t w
 int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* const* const* dA, void* const* const* dB,
                     int flags, void* workspace, size_t ws_bytes, void* hip_stream);
 
+/* ---- Residual stream and norms between two blocks ---------------------------------------------------------------
+ * The blocks above begin with a norm and end with a plain sum.  This is the general step between two blocks of a decoder
+ * whose blocks have a norm behind them too, a learned gate and a scaled residual -- and, with only gamma_pre given, the norm
+ * in front of the vocabulary projection.  For token rows X (the stream), Y (a block's output) [T, d_model], norm(V; gamma) =
+ * V / sqrt(mean(V^2) + eps) * gamma, and token t of job j:
+ *     N = norm(Y; gamma_post);   H = X + res_scale * gate_j * N;   Xn = norm(H; gamma_pre)
+ * gamma_post NULL: N = Y.  gamma_pre NULL: no Xn.  gates NULL, or an entry of it: ones.  X NULL: zeros.  Any of H, Xn may be
+ * NULL (not wanted), not both; Xn is made from the unrounded H.
+ * Backward of L = sum(dH * H) + sum(dXn * Xn); dH or dXn may be NULL (zeros), not both; it reads X and Y, not H:
+ *     D = dH + d norm(H; gamma_pre)^T dXn;   dX = D;   dY = d norm(Y; gamma_post)^T (res_scale * gate_j * D)
+ *     dgamma_pre = sum_t dXn * H rstd_H;   dgamma_post = sum_t res_scale * gate_j * D * Y rstd_Y;
+ *     dgate_j = sum_{t of job j} res_scale * D * N
+ * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs
+ * gamma_post (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or added to with TLORA_BWD_ACCUMULATE (the only flag);
+ * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap no inputs.
+ * tlora_norm_fwd needs no workspace.  tlora_norm_bwd's: 256-byte aligned, tlora_norm_workspace_bytes.  Neither call allocates,
+ * copies or synchronises, so both may be captured into a graph. */
+typedef struct {
+  int32_t dtype;             /* of X, Y, gamma_*, gates, H, Xn and their gradients dX, dY, dH, dXn */
+  int32_t num_jobs, d_model;
+  const int64_t* offsets;    /* HOST [J+1] */
+  float eps, res_scale;
+  const void* X;             /* DEVICE [T, d_model] or NULL */
+  const void* Y;             /* DEVICE [T, d_model] */
+  const void* gamma_post;    /* DEVICE [d_model] or NULL */
+  const void* gamma_pre;     /* DEVICE [d_model] or NULL */
+  const void* const* gates;  /* HOST array of J DEVICE pointers [d_model], or NULL */
+} tlora_norm_t;
+size_t tlora_norm_workspace_bytes(const tlora_norm_t* p);
+int tlora_norm_fwd(const tlora_norm_t* p, void* H, void* Xn, void* hip_stream);
+int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void* dX, void* dY, float* dgamma_post,
+                   float* dgamma_pre, float* const* dgates, int flags, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* ---- Cross entropy of the vocabulary projection ------------------------------------------------------------------
+ * The loss that the jobs' gradients start from (Sec. 3.2: jobs share the backbone, its frozen vocabulary projection included,
+ * and keep their own losses).  For hidden rows H [T, d_model] and W [d_model, ld_w], of which the columns 0 .. vocab - 1 count:
+ *     z_t = H_t . W;   lse_t = log sum_v exp(z_tv);   loss_t = lse_t - z_t,y(t)
+ *     job_loss_j = sum_{t of job j} w_t loss_t / sum_{t of job j} w_t
+ * targets (DEVICE int32 [T]) outside [0, vocab) mark tokens without a loss (prompts, padding): their loss, lse and dH rows are
+ * zero, whatever their H row holds, and they enter no sum.  weights (DEVICE fp32 [T], finite; NULL = ones).  A job whose
+ * weights sum to zero has job_loss 0 and no gradient.
+ * tlora_ce_fwd_bwd also makes  dH_t = g_t (softmax(z_t) - onehot(y_t)) . W^T  with g_t = dloss[t] (DEVICE fp32 [T]) or, with
+ * dloss NULL, of L = sum_j job_loss_j.  W is frozen: no gradient.
+ * Pieces of at most 4096 tokens are taken one after the other, and of a piece the exponentials exp(z) are kept as bf16 between the two
+ * products (half a step of a bf16 number off, as the probabilities of tlora_attention_*); logits are never stored.  Logits, sums and
+ * statistics are fp32.  loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
+ * bf16 only (TLORA_EDTYPE otherwise); d_model a multiple of 8; vocab >= 1, of any size; ld_w a multiple of 8, vocab <= ld_w <=
+ * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned.
+ * The workspace depends on num_jobs, T, d_model, vocab, ld_w and with_grad (0: tlora_ce_fwd, else tlora_ce_fwd_bwd), and never
+ * falls when tokens are added.  Neither call allocates, copies or synchronises, so both may be captured into a graph. */
+typedef struct {
+  int32_t dtype;             /* TLORA_BF16 */
+  int32_t num_jobs, d_model, vocab;
+  int64_t ld_w;
+  const int64_t* offsets;    /* HOST [J+1] */
+  const void* H;             /* DEVICE [T, d_model] */
+  const void* W;             /* DEVICE [d_model, ld_w], never written */
+  const int32_t* targets;    /* DEVICE [T] */
+  const float* weights;      /* DEVICE [T] or NULL */
+} tlora_ce_t;
+size_t tlora_ce_workspace_bytes(const tlora_ce_t* p, int32_t with_grad);
+int tlora_ce_fwd(const tlora_ce_t* p, float* loss, float* lse, float* job_loss, void* workspace, size_t ws_bytes,
+                 void* hip_stream);
+int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float* lse, float* job_loss, void* dH,
+                     void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* ---- Activations kept in 8 bits ------------------------------------------------------------------------------------
+ * What a training step keeps of its layers' inputs until their backward decides how many jobs fit a GPU together.  A row's values are
+ * cut into groups of TLORA_CKPT_GROUP (the last one may be shorter); a group has a scale s, the smallest bf16 number >= 2^-100 with
+ * 127 s >= max |x|, and each value the whole number next to the fp32 quotient x / s (ties to even), which stands for x^ = code * s rounded to the
+ * tensor's dtype: |x^ - x| <= s / 2 and that rounding.  A group with a value that is infinite, not a number, or 2^127 or larger comes
+ * back as NaN.
+ * packed: DEVICE, 256-byte aligned, tlora_ckpt_bytes(T, d): int8 [T, d], then, from the next multiple of 256 bytes on, the scales,
+ * bf16 [T, ceil(d / TLORA_CKPT_GROUP)].  d a multiple of 8 and at most TLORA_MAX_FEATURES, 0 <= T <= TLORA_MAX_TOKENS; X: DEVICE
+ * [T, d] of `dtype`, 16-byte aligned.
+ * tlora_bwd_ckpt is tlora_bwd of the problem whose X are the packed values x^: p->X is not read and may be NULL.  With
+ * TLORA_BWD_REUSE_S the S_j of the tlora_fwd before it on this workspace are taken (made from the X that the forward had), otherwise
+ * S_j = X^_j.A_j.  Its workspace, tlora_ckpt_workspace_bytes, begins with that of tlora_fwd / tlora_bwd of the problem; flags and
+ * everything else as tlora_bwd. */
+#define TLORA_CKPT_GROUP 128
+size_t tlora_ckpt_bytes(int64_t tokens, int32_t d);
+int tlora_ckpt_pack(int32_t dtype, const void* X, int64_t tokens, int32_t d, void* packed, void* hip_stream);
+int tlora_ckpt_unpack(int32_t dtype, const void* packed, int64_t tokens, int32_t d, void* X, void* hip_stream);
+size_t tlora_ckpt_workspace_bytes(const tlora_problem_t* p);
+int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY, void* dX, void* const* dA, void* const* dB,
+                   int flags, void* workspace, size_t ws_bytes, void* hip_stream);
+
 /* ---- General token -> adapter assignment --------------------------------------------------------------------
  * Sec. 3.3 describes the kernel as gathering the tokens of adapter i and scattering the results back to the
  * output tensor.  Here X, Y, dY, dX are in the batch's own (arbitrary) token order, and row_index (DEVICE int32 [T],
@@ -468,7 +555,11 @@ typedef enum {
   TLORA_K_ATTN_FWD = 11,    /* causal attention, forward                        */
   TLORA_K_ATTN_BWD = 12,    /* causal attention, backward (2 kernels)           */
   TLORA_K_ROPE = 13,        /* rotary embedding                                 */
-  TLORA_K_COUNT = 14
+  TLORA_K_HEAD = 14,        /* the two products of the vocabulary projection's loss */
+  TLORA_K_LOSS = 15,        /* the rest of it: token list, statistics, job means    */
+  TLORA_K_NORM = 16,        /* residual stream and norms between two blocks         */
+  TLORA_K_CKPT = 17,        /* activations into 8 bits and back                     */
+  TLORA_K_COUNT = 18
 } tlora_kernel_class_t;
 int tlora_profile(int enable);
 int tlora_profile_read(int kernel_class, double* total_ms, int64_t* launches);

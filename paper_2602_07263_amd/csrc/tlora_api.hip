@@ -2077,6 +2077,391 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
   return tlora_attn_bwd(&L.attn, ws + L.off_dh, dX, dA, dB, flags, ws + L.off_attn, L.ws_attn, hip_stream);
 }
 
+}  // extern "C"
+
+// ---- residual stream and norms between two blocks ------------------------------------------------------------
+namespace tlora {
+namespace {
+constexpr int kNormUnits = 512;               // wanted units of the column sums: two per CU
+struct NormPlan {
+  int64_t T = 0;
+  bool by_job = false;                        // units do not cross jobs
+  int unit_rows = 1;
+  int64_t units = 0;
+  size_t off_rows = 0, off_partial = 0, total = 0;
+};
+int norm_plan(const tlora_norm_t* p, NormPlan& N) {
+  if (!p) return TLORA_ENULL;
+  if (p->dtype != TLORA_F32 && p->dtype != TLORA_BF16) return TLORA_EDTYPE;
+  if (p->num_jobs < 1 || p->num_jobs > TLORA_MAX_JOBS || p->d_model < 8 || p->d_model % 8 || p->d_model > TLORA_MAX_FEATURES)
+    return TLORA_EINVAL;
+  if (!(p->eps >= 0.f) || !std::isfinite(p->eps) || !std::isfinite(p->res_scale)) return TLORA_EINVAL;
+  if (!p->offsets) return TLORA_ENULL;
+  if (p->offsets[0] != 0) return TLORA_EINVAL;
+  for (int j = 0; j < p->num_jobs; ++j)
+    if (p->offsets[j + 1] < p->offsets[j] || p->offsets[j + 1] > TLORA_MAX_TOKENS) return TLORA_EINVAL;
+  N.T = p->offsets[p->num_jobs];
+  N.by_job = p->gates != nullptr;
+  N.unit_rows = (int)std::max<int64_t>(4, (N.T + kNormUnits - 1) / kNormUnits);
+  auto units = [&](int64_t rows) { return (rows + N.unit_rows - 1) / N.unit_rows; };
+  if (N.by_job)
+    for (int j = 0; j < p->num_jobs; ++j) N.units += units(p->offsets[j + 1] - p->offsets[j]);
+  else
+    N.units = units(N.T);
+  size_t w = 0;
+  auto place = [&](size_t bytes) { const size_t at = w;  w = align_up(w + bytes, 256);  return at; };
+  N.off_rows = place(sizeof(float) * 4 * (size_t)N.T);
+  N.off_partial = place(sizeof(float) * 3 * (size_t)N.units * p->d_model);
+  N.total = std::max<size_t>(w, 256);
+  return TLORA_OK;
+}
+int norm_checks(const tlora_norm_t* p, const NormPlan& N) {
+  if (N.T > 0 && !p->Y) return TLORA_ENULL;
+  if (misaligned16(p->X) || misaligned16(p->Y) || misaligned16(p->gamma_post) || misaligned16(p->gamma_pre)) return TLORA_EALIGN;
+  if (p->gates)
+    for (int j = 0; j < p->num_jobs; ++j)
+      if (misaligned16(p->gates[j])) return TLORA_EALIGN;
+  return TLORA_OK;
+}
+NormArgs norm_args(const tlora_norm_t* p) {
+  NormArgs a;
+  a.X = p->X;  a.Y = p->Y;  a.gamma_post = p->gamma_post;  a.gamma_pre = p->gamma_pre;
+  a.eps = p->eps;  a.res_scale = p->res_scale;  a.d = p->d_model;
+  return a;
+}
+// Calls launch(jobs, rows, units) for group after group of jobs that have tokens (with `idle`: of all jobs).  Without gates all
+// tokens are one job.  unit_rows 1: units are rows.
+template <class Launch>
+void norm_groups(const tlora_norm_t* p, const NormPlan& N, int unit_rows, float* const* dgates, bool idle, const Launch& launch) {
+  NormJobs jobs;
+  int rows = 0, units = 0, base = 0;
+  auto flush = [&]() {
+    if (jobs.n) launch(jobs, rows, units);
+    base += units;
+    jobs = NormJobs();
+    jobs.unit_base = base;
+    rows = units = 0;
+  };
+  const int J = N.by_job ? p->num_jobs : 1;
+  for (int j = 0; j < J; ++j) {
+    NormJob jb;
+    jb.row0 = (int32_t)(N.by_job ? p->offsets[j] : 0);
+    jb.row1 = (int32_t)(N.by_job ? p->offsets[j + 1] : N.T);
+    if (jb.row1 == jb.row0 && !idle) continue;
+    jb.gate = N.by_job ? p->gates[j] : nullptr;
+    jb.dgate = dgates ? dgates[j] : nullptr;
+    jb.unit0 = units;
+    jb.units = (jb.row1 - jb.row0 + unit_rows - 1) / unit_rows;
+    rows += jb.row1 - jb.row0;
+    units += jb.units;
+    jobs.job[jobs.n++] = jb;
+    if (jobs.n == kNormJobs) flush();
+  }
+  flush();
+}
+}  // namespace
+}  // namespace tlora
+
+extern "C" {
+
+size_t tlora_norm_workspace_bytes(const tlora_norm_t* p) {
+  NormPlan N;
+  return norm_plan(p, N) == TLORA_OK ? N.total : 0;
+}
+
+int tlora_norm_fwd(const tlora_norm_t* p, void* H, void* Xn, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  NormPlan N;
+  int rc = norm_plan(p, N);
+  if (rc == TLORA_OK) rc = norm_checks(p, N);
+  if (rc != TLORA_OK) return rc;
+  if (N.T > 0 && ((!H && !Xn) || (Xn && !p->gamma_pre))) return TLORA_ENULL;
+  if (misaligned16(H) || misaligned16(Xn)) return TLORA_EALIGN;
+  rc = check_arch();
+  if (rc != TLORA_OK || N.T == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  {
+    Timed t(TLORA_K_NORM, st);
+    norm_groups(p, N, 1, nullptr, false, [&](const NormJobs& jobs, int rows, int) {
+      launch_norm_fwd(p->dtype == TLORA_BF16, norm_args(p), jobs, rows, H, Xn, st);
+    });
+  }
+  return launches_ok(__LINE__);
+}
+
+int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void* dX, void* dY, float* dgamma_post,
+                   float* dgamma_pre, float* const* dgates, int flags, void* workspace, size_t ws_bytes, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  NormPlan N;
+  int rc = norm_plan(p, N);
+  if (rc == TLORA_OK) rc = norm_checks(p, N);
+  if (rc != TLORA_OK) return rc;
+  if (flags & ~TLORA_BWD_ACCUMULATE) return TLORA_EINVAL;
+  if (N.T > 0 && !dH && !dXn) return TLORA_ENULL;
+  if ((dXn && !p->gamma_pre) || (dgamma_pre && !p->gamma_pre) || (dgamma_post && !p->gamma_post) || (dgates && !p->gates))
+    return TLORA_ENULL;
+  if (misaligned16(dH) || misaligned16(dXn) || misaligned16(dX) || misaligned16(dY) || misaligned16(dgamma_post) ||
+      misaligned16(dgamma_pre))
+    return TLORA_EALIGN;
+  bool want_gates = false;
+  if (dgates)
+    for (int j = 0; j < p->num_jobs; ++j) {
+      want_gates = want_gates || dgates[j];
+      if (misaligned16(dgates[j])) return TLORA_EALIGN;
+    }
+  if (bad_ws(workspace, ws_bytes, N.total)) return TLORA_EWORKSPACE;
+  rc = check_arch();
+  if (rc != TLORA_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const bool bf = p->dtype == TLORA_BF16, sums = dgamma_post || dgamma_pre || want_gates;
+  const bool accumulate = (flags & TLORA_BWD_ACCUMULATE) != 0;
+  const NormArgs a = norm_args(p);
+  const NormGrads g = {dH, dXn, dX, dY};
+  float* const rows_at = sums ? reinterpret_cast<float*>(ws + N.off_rows) : nullptr;
+  float* const partial = reinterpret_cast<float*>(ws + N.off_partial);
+  {
+    Timed t(TLORA_K_NORM, st);
+    norm_groups(p, N, 1, nullptr, false,
+                [&](const NormJobs& jobs, int rows, int) { launch_norm_bwd_rows(bf, a, jobs, g, rows, rows_at, st); });
+    if (sums) {
+      norm_groups(p, N, N.unit_rows, nullptr, false, [&](const NormJobs& jobs, int, int units) {
+        launch_norm_bwd_cols(bf, a, jobs, g, units, N.unit_rows, rows_at, partial, st);
+      });
+      // (with `idle` the units are numbered alike: a job without tokens has none)
+      const bool gammas = dgamma_post || dgamma_pre;
+      bool first = true;
+      norm_groups(p, N, N.unit_rows, want_gates ? dgates : nullptr, true, [&](const NormJobs& jobs, int, int) {
+        const int from = first && gammas ? 0 : 2;
+        launch_norm_reduce(partial, jobs, from, 2 - from + (want_gates ? jobs.n : 0), p->d_model, dgamma_post, dgamma_pre,
+                           (int)N.units, accumulate, st);
+        first = false;
+      });
+    }
+  }
+  return launches_ok(__LINE__);
+}
+
+// ---- cross entropy of the vocabulary projection --------------------------------------------------------------
+namespace {
+constexpr int64_t kCePieceRows = 4096;                     // most tokens of a piece with the gradient,
+constexpr int64_t kCeEvalRows = 16384;                     // and of one without
+constexpr int64_t kCePieceElements = (int64_t)1 << 30;     // most elements of its exponentials
+struct CePlan {
+  int64_t T = 0;
+  int piece = 0, col_tiles = 0;
+  size_t off_offsets = 0, off_live = 0, off_list = 0, off_target = 0, off_share = 0, off_loss = 0, off_rows = 0, off_stats = 0,
+         off_logit = 0, off_factor = 0, off_E = 0, off_E_tail = 0, off_W_tail = 0, off_part = 0, total = 0;
+};
+int ce_plan(const tlora_ce_t* p, bool grad, CePlan& C) {
+  if (!p) return TLORA_ENULL;
+  if (p->dtype != TLORA_BF16) return TLORA_EDTYPE;
+  if (p->num_jobs < 1 || p->num_jobs > TLORA_MAX_JOBS || p->d_model < 8 || p->d_model % 8 || p->d_model > TLORA_MAX_FEATURES)
+    return TLORA_EINVAL;
+  if (p->vocab < 1 || p->ld_w < p->vocab || p->ld_w % 8 || p->ld_w > TLORA_MAX_FEATURES) return TLORA_EINVAL;
+  if (!p->offsets) return TLORA_ENULL;
+  if (p->offsets[0] != 0) return TLORA_EINVAL;
+  for (int j = 0; j < p->num_jobs; ++j)
+    if (p->offsets[j + 1] < p->offsets[j] || p->offsets[j + 1] > TLORA_MAX_TOKENS) return TLORA_EINVAL;
+  C.T = p->offsets[p->num_jobs];
+  C.col_tiles = (p->vocab + kGemmBN - 1) / kGemmBN;
+  const int64_t most = grad ? std::max<int64_t>(kGemmBM, std::min(kCePieceRows, kCePieceElements / p->ld_w / kGemmBM * kGemmBM)) : kCeEvalRows;
+  C.piece = (int)std::min<int64_t>(most, (int64_t)align_up((size_t)std::max<int64_t>(C.T, 1), kGemmBM));
+  size_t w = 0;
+  auto place = [&](size_t bytes) { const size_t at = w;  w = align_up(w + bytes, 256);  return at; };
+  const size_t T = (size_t)C.T, n = (size_t)C.piece, d = (size_t)p->d_model;
+  C.off_offsets = place(sizeof(int64_t) * ((size_t)p->num_jobs + 1));
+  C.off_live = place(sizeof(int32_t));
+  C.off_list = place(sizeof(int32_t) * T);
+  C.off_target = place(sizeof(int32_t) * T);
+  C.off_loss = place(sizeof(float) * T);
+  C.off_share = place(grad ? sizeof(float) * T : 0);
+  C.off_rows = place(2 * n * d);
+  C.off_stats = place(sizeof(HeadStat) * n * (size_t)C.col_tiles);
+  C.off_logit = place(sizeof(float) * n);
+  C.off_factor = place(sizeof(float) * n);
+  if (grad) {
+    C.off_E = place(2 * n * (size_t)p->ld_w);
+    C.off_E_tail = place(2 * n * 32);
+    C.off_W_tail = place(2 * d * 32);
+    C.off_part = place(kHeadPartBytes);
+  }
+  C.total = w;
+  return TLORA_OK;
+}
+int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, float* lse, float* job_loss, void* dH, void* workspace,
+           size_t ws_bytes, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  CePlan C;
+  int rc = ce_plan(p, grad, C);
+  if (rc != TLORA_OK) return rc;
+  if (!p->W || (C.T > 0 && (!p->H || !p->targets || (grad && !dH)))) return TLORA_ENULL;
+  if (misaligned16(p->H) || misaligned16(p->W) || misaligned16(dH)) return TLORA_EALIGN;
+  if (bad_ws(workspace, ws_bytes, C.total)) return TLORA_EWORKSPACE;
+  rc = check_arch();
+  if (rc != TLORA_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  const int d = p->d_model, J = p->num_jobs;
+  const uint16_t* const W = static_cast<const uint16_t*>(p->W);
+  CeTokens c;
+  c.T = (int32_t)C.T;  c.vocab = p->vocab;
+  c.offsets = reinterpret_cast<const int64_t*>(ws + C.off_offsets);
+  c.targets = p->targets;  c.weights = p->weights;
+  c.live = reinterpret_cast<int32_t*>(ws + C.off_live);
+  c.list = reinterpret_cast<int32_t*>(ws + C.off_list);
+  c.target = reinterpret_cast<int32_t*>(ws + C.off_target);
+  c.share = grad ? reinterpret_cast<float*>(ws + C.off_share) : nullptr;
+  c.token_loss = reinterpret_cast<float*>(ws + C.off_loss);
+  uint16_t* const E = grad ? reinterpret_cast<uint16_t*>(ws + C.off_E) : nullptr;
+  uint16_t* const E_tail = reinterpret_cast<uint16_t*>(ws + C.off_E_tail);
+  uint16_t* const W_tail = reinterpret_cast<uint16_t*>(ws + C.off_W_tail);
+  uint16_t* const rows = reinterpret_cast<uint16_t*>(ws + C.off_rows);
+  {
+    Timed t(TLORA_K_LOSS, st);
+    launch_table_write(p->offsets, sizeof(int64_t) * ((size_t)J + 1), ws + C.off_offsets, st);
+    launch_ce_prepare(c, J, dloss, loss, lse, st);
+    if (grad) launch_ce_zero_rows(c, static_cast<uint16_t*>(dH), d, st);
+    if (grad && p->vocab % 32) launch_ce_tail(W, p->ld_w, d, p->vocab, W_tail, st);
+  }
+  for (int64_t first = 0; first < C.T; first += C.piece) {
+    HeadParams h;
+    h.live = c.live;  h.first = (int)first;  h.max_rows = (int)std::min<int64_t>(C.piece, C.T - first);
+    h.vocab = p->vocab;  h.ld = (int)p->ld_w;  h.col_tiles = C.col_tiles;
+    h.target = c.target + first;
+    h.target_logit = reinterpret_cast<float*>(ws + C.off_logit);
+    h.stats = reinterpret_cast<HeadStat*>(ws + C.off_stats);
+    float* const factor = reinterpret_cast<float*>(ws + C.off_factor);
+    h.factor = factor;
+    {
+      Timed t(TLORA_K_LOSS, st);
+      launch_ce_gather(h, c, static_cast<const uint16_t*>(p->H), rows, d, st);
+    }
+    {
+      Timed t(TLORA_K_HEAD, st);
+      launch_head_logits(h, rows, W, E, d, st);
+    }
+    {
+      Timed t(TLORA_K_LOSS, st);
+      launch_ce_finish(h, c, E, E_tail, factor, loss, lse, st);
+    }
+    if (grad) {
+      Timed t(TLORA_K_HEAD, st);
+      launch_head_grad(h, E, E_tail, W, W_tail, static_cast<uint16_t*>(dH), c.list + first, d,
+                       reinterpret_cast<float*>(ws + C.off_part), st);
+    }
+  }
+  if (job_loss) {
+    Timed t(TLORA_K_LOSS, st);
+    launch_ce_jobs(c, J, job_loss, st);
+  }
+  return launches_ok(__LINE__);
+}
+}  // namespace
+
+size_t tlora_ce_workspace_bytes(const tlora_ce_t* p, int32_t with_grad) {
+  CePlan C;
+  return ce_plan(p, with_grad != 0, C) == TLORA_OK ? C.total : 0;
+}
+int tlora_ce_fwd(const tlora_ce_t* p, float* loss, float* lse, float* job_loss, void* workspace, size_t ws_bytes, void* hip_stream) {
+  return ce_run(p, false, nullptr, loss, lse, job_loss, nullptr, workspace, ws_bytes, hip_stream);
+}
+int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float* lse, float* job_loss, void* dH, void* workspace,
+                     size_t ws_bytes, void* hip_stream) {
+  return ce_run(p, true, dloss, loss, lse, job_loss, dH, workspace, ws_bytes, hip_stream);
+}
+
+// ---- activations kept in 8 bits ------------------------------------------------------------------------------
+namespace {
+int ckpt_sizes(int64_t tokens, int32_t d) {
+  if (tokens < 0 || tokens > TLORA_MAX_TOKENS || d < 8 || d % 8 || d > TLORA_MAX_FEATURES) return TLORA_EINVAL;
+  const int64_t groups = (d + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
+  return tokens * groups <= (int64_t)1 << 34 ? TLORA_OK : TLORA_EINVAL;       // a workgroup per 16 groups
+}
+size_t ckpt_scales_at(int64_t tokens, int32_t d) { return align_up((size_t)tokens * (size_t)d, 256); }
+int ckpt_checks(int32_t dtype, const void* X, int64_t tokens, int32_t d, const void* packed) {
+  if (dtype != TLORA_F32 && dtype != TLORA_BF16) return TLORA_EDTYPE;
+  const int rc = ckpt_sizes(tokens, d);
+  if (rc != TLORA_OK) return rc;
+  if (tokens > 0 && (!X || !packed)) return TLORA_ENULL;
+  if (misaligned16(X) || (reinterpret_cast<uintptr_t>(packed) & 255)) return TLORA_EALIGN;
+  return check_arch();
+}
+}  // namespace
+
+size_t tlora_ckpt_bytes(int64_t tokens, int32_t d) {
+  if (ckpt_sizes(tokens, d) != TLORA_OK) return 0;
+  const size_t groups = (size_t)(d + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
+  return std::max<size_t>(256, align_up(ckpt_scales_at(tokens, d) + 2 * (size_t)tokens * groups, 256));
+}
+
+int tlora_ckpt_pack(int32_t dtype, const void* X, int64_t tokens, int32_t d, void* packed, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  const int rc = ckpt_checks(dtype, X, tokens, d, packed);
+  if (rc != TLORA_OK || tokens == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  uint8_t* const codes = static_cast<uint8_t*>(packed);
+  {
+    Timed t(TLORA_K_CKPT, st);
+    launch_ckpt_pack(dtype == TLORA_BF16, X, tokens, d, codes, reinterpret_cast<uint16_t*>(codes + ckpt_scales_at(tokens, d)), st);
+  }
+  return launches_ok(__LINE__);
+}
+
+int tlora_ckpt_unpack(int32_t dtype, const void* packed, int64_t tokens, int32_t d, void* X, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  const int rc = ckpt_checks(dtype, X, tokens, d, packed);
+  if (rc != TLORA_OK || tokens == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const uint8_t* const codes = static_cast<const uint8_t*>(packed);
+  {
+    Timed t(TLORA_K_CKPT, st);
+    launch_ckpt_unpack(dtype == TLORA_BF16, codes, reinterpret_cast<const uint16_t*>(codes + ckpt_scales_at(tokens, d)), tokens, d, X, st);
+  }
+  return launches_ok(__LINE__);
+}
+
+size_t tlora_ckpt_workspace_bytes(const tlora_problem_t* p) {
+  const size_t inner = tlora_workspace_bytes(p);
+  if (inner == 0 || ckpt_sizes(p->offsets[p->num_jobs], p->d_in) != TLORA_OK) return 0;
+  const size_t elt = p->dtype == TLORA_F32 ? 4 : 2;
+  return align_up(align_up(inner, 256) + elt * (size_t)p->offsets[p->num_jobs] * (size_t)p->d_in, 256);
+}
+
+int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY, void* dX, void* const* dA, void* const* dB,
+                   int flags, void* workspace, size_t ws_bytes, void* hip_stream) {
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  int rc = validate(p);
+  if (rc != TLORA_OK) return rc;
+  const int64_t T = p->offsets[p->num_jobs];
+  rc = ckpt_sizes(T, p->d_in);
+  if (rc != TLORA_OK) return rc;
+  const size_t need = tlora_ckpt_workspace_bytes(p), inner = align_up(tlora_workspace_bytes(p), 256);
+  if (bad_ws(workspace, ws_bytes, need)) return TLORA_EWORKSPACE;
+  if (T > 0 && !packed) return TLORA_ENULL;
+  if (reinterpret_cast<uintptr_t>(packed) & 255) return TLORA_EALIGN;
+  tlora_problem_t q = *p;
+  uint8_t* const X = static_cast<uint8_t*>(workspace) + inner;
+  q.X = X;
+  // (everything is checked before the first launch)
+  const PlanEntry* entry = nullptr;
+  std::vector<JobDev> hjobs;
+  rc = common_checks(&q, &entry, hjobs, workspace, inner);
+  if (rc != TLORA_OK) return rc;
+  if (T > 0 && !dY) return TLORA_ENULL;
+  if ((dA == nullptr) != (dB == nullptr)) return TLORA_ENULL;
+  if (misaligned16(dY) || misaligned16(dX)) return TLORA_EALIGN;
+  if (dA)
+    for (int j = 0; j < p->num_jobs; ++j)
+      if (p->ranks[j] > 0 && (!dA[j] || !dB[j])) return TLORA_ENULL;
+  if (flags & ~(TLORA_BWD_REUSE_S | TLORA_BWD_REUSE_WT | TLORA_BWD_ACCUMULATE)) return TLORA_EINVAL;
+  if (dA) {                       // (X enters the adapters' gradients alone)
+    rc = tlora_ckpt_unpack(p->dtype, packed, T, p->d_in, X, hip_stream);
+    if (rc != TLORA_OK) return rc;
+  }
+  return tlora_bwd(&q, dY, dX, dA, dB, flags, workspace, inner, hip_stream);
+}
+
 // ---- general token -> adapter assignment (Sec. 3.3: tokens of an adapter are gathered, results scattered back) ----
 namespace {
 struct IndexedLayout {

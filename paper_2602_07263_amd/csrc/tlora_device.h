@@ -1,0 +1,59 @@
+// Device helpers that several kernel files share: vector types, 16-byte accesses, conversions, sums.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tlora {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ u32x4 ldg16(const void* p) { return *reinterpret_cast<const u32x4*>(p); }
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 v = {(__bf16)lo, (__bf16)hi};   // round-to-nearest-even
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float bf16_float(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
+
+// Eight consecutive elements from i on (16-byte aligned), bf16 (BF) or fp32.
+template <bool BF>
+__device__ __forceinline__ void load8(const void* p, int64_t i, float (&v)[8]) {
+  if (BF) {
+    const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __builtin_bit_cast(float, r[e] << 16);
+      v[2 * e + 1] = __builtin_bit_cast(float, r[e] & 0xffff0000u);
+    }
+  } else {
+    const f32x4* f = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+    const f32x4 a = f[0], b = f[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = a[e];  v[4 + e] = b[e]; }
+  }
+}
+template <bool BF>
+__device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[8]) {
+  if (BF) {
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + i) =
+        u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  } else {
+    f32x4* f = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
+    f[0] = f32x4{v[0], v[1], v[2], v[3]};
+    f[1] = f32x4{v[4], v[5], v[6], v[7]};
+  }
+}
+// sum over the 256 threads of a workgroup (every thread gets the total)
+__device__ __forceinline__ float block_sum(float x, float* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  const float t = red[0] + red[1] + red[2] + red[3];
+  __syncthreads();
+  return t;
+}
+
+}  // namespace tlora

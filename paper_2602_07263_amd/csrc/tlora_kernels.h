@@ -107,6 +107,92 @@ void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, 
 void launch_grad_reduce(const JobDev* jobs, const GradGroup* groups, int num_groups, const float* partial, int D,
                         bool out_is_dA, bool accumulate, hipStream_t st);
 
+// ---- cross entropy of the vocabulary projection (bf16) ----------------------------------------------------------------------
+// The tokens that have a loss are listed first (`live`, in token order); everything after works on pieces of the list, `max_rows` rows
+// from place `first` on, of which those before *live exist: the host does not know their number, so grids are sized for a full piece.
+struct HeadStat {
+  float ref, sum;                        // of a row's logits z in a tile of kGemmBN columns: sum of exp(z - ref)
+};
+struct HeadParams {
+  const int32_t* live = nullptr;         // how many tokens the list has
+  int first = 0, max_rows = 0;
+  int vocab = 0, ld = 0, kext = 0;       // columns that count; elements per row of W and of E; K-steps behind the last whole one (0 | 32)
+  int col_tiles = 0;                     // tiles of kGemmBN columns
+  const int32_t* target = nullptr;       // [max_rows] of the piece
+  float* target_logit = nullptr;         // [max_rows]
+  HeadStat* stats = nullptr;             // [max_rows, col_tiles]
+  const float* factor = nullptr;         // [max_rows] what a row of E W^T is multiplied by
+};
+constexpr int kHeadMaxSplits = 16;
+constexpr size_t kHeadPartBytes = (size_t)256 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most one round of tiles
+// Largest logit of a row in a tile up to which exp(z) needs no reference, and from which on sums of it hold their digits.
+__host__ __device__ inline float head_reference(float m) {
+  constexpr float kTop = 60.f, kBottom = -40.f;
+  return m <= kTop && m >= kBottom ? 0.f : m == -__builtin_huge_valf() ? 0.f : m;
+}
+// E = exp(H.W - ref) as bf16 [max_rows, ld] (null: statistics alone), zero from vocab to the next multiple of 8; stats; target_logit.
+void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, hipStream_t st);
+// dH[out_index[r]] = factor[r] * (E[r] . W^T).  The columns from vocab / 32 * 32 on come from E_tail [max_rows padded to 256, 32] and
+// W_tail [d, 32] (null if there are none).  part: kHeadPartBytes.
+void launch_head_grad(const HeadParams& head, const uint16_t* E, const uint16_t* E_tail, const uint16_t* W, const uint16_t* W_tail,
+                      uint16_t* dH, const int32_t* out_index, int d, float* part, hipStream_t st);
+
+// The rest of the loss.
+struct CeTokens {
+  int32_t T = 0, vocab = 0;
+  const int64_t* offsets = nullptr;      // [J + 1]
+  const int32_t* targets = nullptr;      // [T]
+  const float* weights = nullptr;        // [T] or null: ones
+  int32_t *live = nullptr, *list = nullptr, *target = nullptr;    // the list of the tokens with a loss, and their targets
+  float* share = nullptr;                // [T] what a token's loss counts for; null: no gradient
+  float* token_loss = nullptr;           // [T]; written for the tokens with a loss
+};
+// The list, the shares (dloss instead of them if given), zeros in loss and lse (either may be null) of the other tokens.
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const float* dloss, float* loss, float* lse, hipStream_t st);
+void launch_ce_gather(const HeadParams& h, const CeTokens& c, const uint16_t* H, uint16_t* rows, int d, hipStream_t st);
+void launch_ce_zero_rows(const CeTokens& c, uint16_t* dH, int d, hipStream_t st);
+void launch_ce_tail(const uint16_t* W, int64_t ld, int d, int vocab, uint16_t* tail, hipStream_t st);
+// Statistics -> losses; E null: no gradient.
+void launch_ce_finish(const HeadParams& h, const CeTokens& c, uint16_t* E, uint16_t* E_tail, float* factor, float* loss, float* lse,
+                      hipStream_t st);
+void launch_ce_jobs(const CeTokens& c, int num_jobs, float* job_loss, hipStream_t st);
+
+// ---- residual stream and norms between two blocks -----------------------------------------------------------------------------
+struct NormArgs {
+  const void *X = nullptr, *Y = nullptr, *gamma_post = nullptr, *gamma_pre = nullptr;
+  float eps = 0.f, res_scale = 1.f;
+  int d = 0;
+};
+struct NormGrads {
+  const void *dH = nullptr, *dXn = nullptr;
+  void *dX = nullptr, *dY = nullptr;
+};
+struct NormJob {
+  int32_t row0 = 0, row1 = 0;
+  int32_t unit0 = 0, units = 0;          // of the launch
+  const void* gate = nullptr;
+  float* dgate = nullptr;
+};
+constexpr int kNormJobs = 96;            // jobs of a launch: they travel as its argument
+struct NormJobs {
+  int32_t n = 0;
+  int32_t unit_base = 0;                 // units of the launches before this one
+  NormJob job[kNormJobs];
+};
+void launch_norm_fwd(bool bf16, const NormArgs& a, const NormJobs& jobs, int rows, void* H, void* Xn, hipStream_t st);
+// row_stats: 4 floats per row, or null: not wanted
+void launch_norm_bwd_rows(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int rows, float* row_stats,
+                          hipStream_t st);
+// partial [units of all launches][3][d]
+void launch_norm_bwd_cols(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int units, int unit_rows,
+                          const float* row_stats, float* partial, hipStream_t st);
+void launch_norm_reduce(const float* partial, const NormJobs& jobs, int first_vector, int vectors, int d, float* gamma_post,
+                        float* gamma_pre, int all_units, bool accumulate, hipStream_t st);
+
+// ---- activations in 8 bits ------------------------------------------------------------------------------------------------------
+void launch_ckpt_pack(bool bf16, const void* X, int64_t T, int d, uint8_t* codes, uint16_t* scales, hipStream_t st);
+void launch_ckpt_unpack(bool bf16, const uint8_t* codes, const uint16_t* scales, int64_t T, int d, void* X, hipStream_t st);
+
 // fp32 configuration: strided products on plain FMA units.
 void launch_f32_units(const F32Unit* units, const F32Tile* tiles, int num_tiles, hipStream_t st);
 

@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "tlora_device.h"
 #include "tlora_kernels.h"
 
 namespace tlora {
@@ -20,10 +21,7 @@ namespace tlora {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T*)(p))
 
@@ -36,12 +34,6 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-__device__ __forceinline__ u32x4 ldg16(const void* p) { return *reinterpret_cast<const u32x4*>(p); }
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  bf16x2 v = {(__bf16)lo, (__bf16)hi};   // round-to-nearest-even
-  return __builtin_bit_cast(uint32_t, v);
-}
 
 // Asynchronous 16-byte-per-lane global->LDS load issued as raw instructions: lane l's 16 bytes land at LDS
 // byte address `lds_base` + 16 l (lds_base wave-uniform; it travels in M0).  Unlike the compiler builtin this
@@ -934,6 +926,26 @@ void launch_shrink_stream(const JobDev* jobs, const TileDev* tiles, const Shrink
 // operand is fetched as a whole 128-byte line: the same bytes in half as many L2 requests (a load-only
 // replica of the two streams sustains ~15.4 TB/s this way against ~11.5 TB/s).
 // ---------------------------------------------------------------------------------------------------
+enum { kHeadNone = 0, kHeadLogits = 1, kHeadGrad = 2 };
+struct HeadShape {
+  int rows, tiles_m;
+  GemmSplit split;
+};
+// Rows of the piece that are there, and how the gradient's tiles are cut: whole rounds of 256 tiles (the chip's CUs) as they are,
+// the rest into as many shares as fill one round, each of 32 K-steps at least.
+__device__ __forceinline__ HeadShape head_shape(const HeadParams& h, bool cut, int tiles_n, int steps) {
+  HeadShape s;
+  s.rows = __builtin_amdgcn_readfirstlane(min(max(*h.live - h.first, 0), h.max_rows));
+  s.tiles_m = (s.rows + kGemmBM - 1) / kGemmBM;
+  const int tiles = s.tiles_m * tiles_n, rest = tiles & 255;
+  s.split.n_direct = tiles;
+  if (cut && rest) {
+    s.split.splits = __builtin_amdgcn_readfirstlane(max(1, min(min(256 / rest, kHeadMaxSplits), steps / 32)));
+    if (s.split.splits > 1) s.split.n_direct = tiles - rest;
+  }
+  return s;
+}
+
 struct GemmParams {
   const TileDev* tiles;
   const uint16_t* act;      // [T, K]
@@ -954,6 +966,8 @@ struct GemmParams {
   // a second product of the same shape behind the first in the walk, if n_tiles is twice tiles_m tiles_n
   int n_tiles;
   GemmOperands second;
+  // HEAD instantiations
+  HeadParams head;
 };
 
 // Tile L of the walk: groups of 4 row tiles, so that workgroups that run together share activation and weight panels.
@@ -969,6 +983,60 @@ __device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, in
   tn = __builtin_amdgcn_readfirstlane(Lg / gsize);
 }
 
+// What a tile of logits leaves of itself.  A lane holds tokens 16 i + l % 16 of its wave's 128 rows and features 4 (l / 16) .. + 3 of
+// each of the wave's four blocks of 16 columns.  The row's exponentials are taken relative to 0 where its largest logit in the tile
+// lies within kHeadPlain, so that the tiles of a row agree on the reference and the gradient's product can add them up as they are;
+// a bf16 exponential has the same 8 significant bits at any size.  Outside of that the reference is the largest logit itself.
+// scratch: 2 x 4 x 256 floats.
+__device__ __forceinline__ void head_softmax_tile(const HeadParams& h, f32x4 (&acc)[4][8], float* scratch, int row0, int rows_valid, int tn,
+                                                  int wm, int wn, int lane, int tid) {
+  constexpr float kLog2e = 1.44269504088896340736f;
+  const int c0 = tn * kGemmBN + wn * 64 + (lane >> 4) * 4;       // the lane's first column
+  float* const wmax = scratch;
+  float* const wsum = scratch + 4 * kGemmBM;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float m = -__builtin_huge_valf();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c0 + j * 16 + e < h.vocab) m = fmaxf(m, acc[j][i][e]);
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    if (lane < 16) wmax[wn * kGemmBM + wm * 128 + i * 16 + lane] = m;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int R = wm * 128 + i * 16 + (lane & 15);
+    const float m = fmaxf(fmaxf(wmax[R], wmax[kGemmBM + R]), fmaxf(wmax[2 * kGemmBM + R], wmax[3 * kGemmBM + R]));
+    const float ref = head_reference(m);
+    const int y = R < rows_valid ? h.target[row0 + R] - c0 : -1;   // the target's column among the lane's, if it is one of them
+    float s = 0.f, zy = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = acc[j][i][e];
+        if (y == j * 16 + e) zy = z;
+        const float x = c0 + j * 16 + e < h.vocab ? __builtin_amdgcn_exp2f((z - ref) * kLog2e) : 0.f;
+        acc[j][i][e] = x;
+        s += x;
+      }
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    if (lane < 16) wsum[wn * kGemmBM + R] = s;
+    if (y >= 0 && y < 64 && (y & 15) < 4) h.target_logit[row0 + R] = zy;
+  }
+  __syncthreads();
+  if (tid < rows_valid) {
+    const float m = fmaxf(fmaxf(wmax[tid], wmax[kGemmBM + tid]), fmaxf(wmax[2 * kGemmBM + tid], wmax[3 * kGemmBM + tid]));
+    const float s = (wsum[tid] + wsum[kGemmBM + tid]) + (wsum[2 * kGemmBM + tid] + wsum[3 * kGemmBM + tid]);
+    h.stats[(int64_t)(row0 + tid) * h.col_tiles + tn] = HeadStat{head_reference(m), s};
+  }
+}
+
 // KTAIL: the instantiation for K % 32 != 0 carries the extra predicated step; keeping it out of the common one
 // keeps its register pressure away from every tile.
 // INDEXED: the activation rows are fetched through P.in_index (token-indexed calls: the batch stays in its own order).
@@ -976,7 +1044,10 @@ __device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, in
 // 32 bits, so the launcher takes this instantiation only while T * K * 2 stays below 4 GiB.
 // SPLIT: the last tiles of the walk, which would occupy fewer workgroups than the chip has CUs for a whole contraction,
 // are cut along K (gemm_split in the planner says when); gemm_reduce_kernel adds the sums in split order.
-template <bool KN, bool KTAIL, bool INDEXED, bool SPLIT>
+// HEAD: the two products of the vocabulary projection's cross entropy (see HeadParams), of as many rows as the device counts and
+// with no job table.  kHeadLogits: out = exp(logits - reference) as bf16 and the tile's softmax statistics.  kHeadGrad: act is
+// that output, whose rows and those of W have P.head.ld elements, and a row of out is scaled by head.factor.
+template <bool KN, bool KTAIL, bool INDEXED, bool SPLIT, int HEAD = kHeadNone>
 __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
   constexpr int NT = 512;                            // threads: 8 waves
   constexpr int NFB = 4;                             // 16-wide feature blocks per wave (64 columns)
@@ -1005,6 +1076,12 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
   int tm, tn;
   bool cut = false, second;
   int split = 0, tail_tile = 0;
+  if (HEAD) {
+    const HeadShape h = head_shape(P.head, HEAD == kHeadGrad, P.tiles_n, (P.K + P.head.kext) / 32);
+    P.T = h.rows;  P.tiles_m = h.tiles_m;  P.n_tiles = h.tiles_m * P.tiles_n;
+    P.n_direct = h.split.n_direct;  P.splits = h.split.splits;
+    if ((int)blockIdx.x >= (SPLIT ? P.n_direct + (P.n_tiles - P.n_direct) * P.splits : P.n_tiles)) return;
+  }
   {
     const int nb = P.n_tiles, b = blockIdx.x;
     cut = SPLIT && b >= P.n_direct;
@@ -1017,13 +1094,17 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
       tail_tile = __builtin_amdgcn_readfirstlane(L - split * (nb - first));
       L = first + tail_tile;
     }
-    second = L >= P.tiles_m * P.tiles_n;
+    second = !HEAD && L >= P.tiles_m * P.tiles_n;
     if (second) L -= P.tiles_m * P.tiles_n;
     gemm_tile_of(L, P.tiles_m, P.tiles_n, tm, tn);
   }
   const int row0 = tm * BM, col0 = tn * BN;
   const int rows_valid = min(BM, P.T - row0);
-  const TileDev td = P.tiles[tm];
+  const TileDev td = HEAD == kHeadLogits ? TileDev{0, 0, 0, 0, 0}
+                     : HEAD == kHeadGrad ? TileDev{0, 0, P.head.kext, 0, (int64_t)row0 * P.head.kext} : P.tiles[tm];
+  // row strides: of a k-contiguous operand's rows, and of the forward weight's
+  const int lk = HEAD == kHeadGrad ? P.head.ld : P.K;
+  const int ln_ = HEAD == kHeadLogits ? P.head.ld : P.N;
 
   // 16 x 16 x 32 MFMAs: with dense random operands the chip sustains ~15 % more of them per second than of the
   // 32 x 32 x 16 shape under its power limit (half the accumulator traffic per flop).
@@ -1050,7 +1131,7 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
     step0 = min(split * share, ntot);
     step1 = min(step0 + share, ntot);
   }
-  const bool clocked = P.clk != nullptr && (blockIdx.x & 63) == 0;   // a sample of workgroups across the grid
+  const bool clocked = !HEAD && P.clk != nullptr && (blockIdx.x & 63) == 0;   // a sample of workgroups across the grid
   unsigned long long cyc0 = 0, tick0 = 0;
   if (clocked) { cyc0 = __builtin_readcyclecounter();  tick0 = __builtin_amdgcn_s_memrealtime(); }
   if (step1 > step0) {
@@ -1074,9 +1155,9 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
     const uint16_t* const act = second ? P.second.act : P.act;
     const uint16_t* const W = second ? P.second.W : P.W;
     const uint16_t* const packed = second ? P.second.packed : P.packed;
-    const char* const a_base = uniform_ptr(reinterpret_cast<const char*>(INDEXED ? act : act + (int64_t)row0 * P.K));
+    const char* const a_base = uniform_ptr(reinterpret_cast<const char*>(INDEXED ? act : act + (int64_t)row0 * lk));
     const char* const x_base = uniform_ptr(reinterpret_cast<const char*>((second ? P.second.Sx : P.Sx) + td.aoff) - (int64_t)nfull * 64);
-    const char* const w_base = uniform_ptr(reinterpret_cast<const char*>(KN ? W + col0 : W + (int64_t)col0 * P.K));
+    const char* const w_base = uniform_ptr(reinterpret_cast<const char*>(KN ? W + col0 : W + (int64_t)col0 * lk));
     const char* const e_base = uniform_ptr(
         KN ? reinterpret_cast<const char*>(packed + (int64_t)td.roff_first * P.N + col0) - (int64_t)nfull * 64 * P.N
            : reinterpret_cast<const char*>(packed + (int64_t)col0 * P.ra + td.roff_first) - (int64_t)nfull * 64);
@@ -1090,10 +1171,10 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
     uint32_t k_off[2], kn_off[2];
 #pragma unroll
     for (int par = 0; par < 2; ++par) {
-      k_off[par] = (uint32_t)lr * (uint32_t)(P.K * 2) + coff + (h0 ^ par) * 64;       // rows of K elements: act, NT weight
+      k_off[par] = (uint32_t)lr * (uint32_t)(lk * 2) + coff + (h0 ^ par) * 64;       // rows of lk elements: act, NT weight
       const int kl = wave * 8 + par * 2 + (lane >> 5);                                // forward weight: k-row of i = par
       const int c = (lane & 31) ^ ((kl & 3) << 2) ^ (((kl >> 3) & 1) << 1);
-      kn_off[par] = KN ? (uint32_t)(kl & 31) * (uint32_t)(P.N * 2) + c * 16 : 0u;
+      kn_off[par] = KN ? (uint32_t)(kl & 31) * (uint32_t)(ln_ * 2) + c * 16 : 0u;
     }
     // INDEXED: byte offset (from P.act) of the batch row behind each of the lane's four tile rows, chunk and half
     // included; rows beyond the problem edge repeat the last valid one
@@ -1112,19 +1193,19 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
       } else if (!INDEXED && tq < a_plain) {
         const char* const sb = a_base + (int64_t)tq * 64;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dma16s(k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * P.K), dst + i * 1024);
+        for (int i = 0; i < 4; ++i) dma16s(k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * lk), dst + i * 1024);
       } else if (!INDEXED && tq + 1 < nfull) {                 // the last row tile, ragged
         const char* const sb = a_base + (int64_t)tq * 64;
         int below = rows_valid;
         asm volatile("" : "+s"(below));        // (four limits kept through the loop would spill)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          dma16s_below(lane, (below - wave * 32 - i * 8) * 8, k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * P.K), dst + i * 1024);
+          dma16s_below(lane, (below - wave * 32 - i * 8) * 8, k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * lk), dst + i * 1024);
       } else if (!INDEXED && tq >= nfull && tq + 1 < ntot) {   // (INDEXED keeps no offsets for these few steps: general path)
         const char* const sb = x_base + (int64_t)tq * 64;
         int l0 = lane;
         asm volatile("" : "+v"(l0));          // (rows of the adapter operand: found here rather than kept)
-        const uint32_t back = (uint32_t)(wave * 32 + (l0 >> 3)) * (uint32_t)((P.K - td.kext) * 2);
+        const uint32_t back = (uint32_t)(wave * 32 + (l0 >> 3)) * (uint32_t)((lk - td.kext) * 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) dma16s(k_off[i & 1] - back, uniform_ptr(sb + (int64_t)i * 16 * td.kext), dst + i * 1024);
       } else {
@@ -1139,7 +1220,7 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
           const bool ext = t >= nfull;
           const uint32_t off = (ext ? (uint32_t)r * (uint32_t)(td.kext * 2)
                                 : INDEXED ? g_off[i] - coff0 - (h00 ^ (i & 1)) * 64
-                                          : (uint32_t)min(r, rows_valid - 1) * (uint32_t)(P.K * 2)) + t * 64 + coff0;
+                                          : (uint32_t)min(r, rows_valid - 1) * (uint32_t)(lk * 2)) + t * 64 + coff0;
           dma16((ext ? x_base : a_base) + off, dst + i * 1024);
         }
       }
@@ -1150,11 +1231,11 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
         //  "kn16 tile": slot p -> k-row p / 32 (0..63), chunk (p % 32) ^ swizzle(k-row); a wave's rows all belong
         //  to one step, so base and step clamping are wave-uniform
         const int t = min(max(tq + (wave >> 2), 0), ntot - 1);
-        const char* const sb = (t >= nfull ? e_base : w_base) + (int64_t)t * 64 * P.N;
+        const char* const sb = (t >= nfull ? e_base : w_base) + (int64_t)t * 64 * ln_;
         if (t < w_plain) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            dma16s(kn_off[i & 1], uniform_ptr(sb + (int64_t)(i >> 1) * 8 * P.N), dst + i * 1024);   // i / 2: 4 k-rows on
+            dma16s(kn_off[i & 1], uniform_ptr(sb + (int64_t)(i >> 1) * 8 * ln_), dst + i * 1024);   // i / 2: 4 k-rows on
         } else {
           int ln = lane;
           asm volatile("" : "+v"(ln));
@@ -1162,20 +1243,20 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
           for (int i = 0; i < 4; ++i) {
             const int kl = wave * 8 + i * 2 + (ln >> 5);
             const int c = (ln & 31) ^ ((kl & 3) << 2) ^ (((kl >> 3) & 1) << 1);
-            dma16(sb + (int64_t)(kl & 31) * (P.N * 2) + min(c * 16, (P.N - 8 - col0) * 2), dst + i * 1024);
+            dma16(sb + (int64_t)(kl & 31) * (ln_ * 2) + min(c * 16, (P.N - 8 - col0) * 2), dst + i * 1024);
           }
         }
       } else if ((uint32_t)tq < (uint32_t)w_plain) {       // (not the half tile in front of the first step)
         const char* const sb = w_base + (int64_t)tq * 64;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dma16s(k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * P.K), dst + i * 1024);
+        for (int i = 0; i < 4; ++i) dma16s(k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * lk), dst + i * 1024);
       } else if (tq >= 0 && tq + 1 < nfull) {
         const char* const sb = w_base + (int64_t)tq * 64;
         int below = P.N - col0;
         asm volatile("" : "+s"(below));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          dma16s_below(lane, (below - wave * 32 - i * 8) * 8, k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * P.K), dst + i * 1024);
+          dma16s_below(lane, (below - wave * 32 - i * 8) * 8, k_off[i & 1], uniform_ptr(sb + (int64_t)i * 16 * lk), dst + i * 1024);
       } else {                                // the few adapter steps of the backward weight operand included
         int l0 = lane;
         asm volatile("" : "+v"(l0));
@@ -1186,7 +1267,7 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
           const int n = min(r0 + i * 8, P.N - 1 - col0);
           const int t = min(max(tq + (h00 ^ (i & 1)), 0), ntot - 1);
           const bool ext = t >= nfull;
-          const uint32_t off = (uint32_t)n * (uint32_t)((ext ? P.ra : P.K) * 2) + t * 64 + coff0;
+          const uint32_t off = (uint32_t)n * (uint32_t)((ext ? P.ra : lk) * 2) + t * 64 + coff0;
           dma16((ext ? e_base : w_base) + off, dst + i * 1024);
         }
       }
@@ -1295,7 +1376,7 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
       if (KN) {
         const int k = id >> 5, cc = id & 31;
         const bool okb = k < kvalid && col0 + cc * 8 < P.N;
-        breg[i] = okb ? ldg16(P.W + (int64_t)(k0 + k) * P.N + col0 + cc * 8) : u32x4{0, 0, 0, 0};
+        breg[i] = okb ? ldg16(P.W + (int64_t)(k0 + k) * ln_ + col0 + cc * 8) : u32x4{0, 0, 0, 0};
       } else {
         const bool okb = col0 + r < P.N && c * 8 < kvalid;
         breg[i] = okb ? ldg16(P.W + (int64_t)(col0 + r) * P.K + k0 + c * 8) : u32x4{0, 0, 0, 0};
@@ -1336,11 +1417,26 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
     return;
   }
 
+  int le = lane;
+  asm volatile("" : "+v"(le));               // (nothing that only the epilogue needs stays live through the loop)
+  if constexpr (HEAD == kHeadLogits) {
+    __syncthreads();
+    head_softmax_tile(P.head, acc, reinterpret_cast<float*>(lds + 4 * SLOT), row0, rows_valid, tn, wm, wn, le, tid);
+    if (!P.out) return;
+  }
+  if constexpr (HEAD == kHeadGrad) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = P.head.factor[row0 + min(wm * 128 + i * 16 + (le & 15), rows_valid - 1)];
+#pragma unroll
+      for (int j = 0; j < NFB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][i][e] = f == 0.f ? 0.f : acc[j][i][e] * f;
+    }
+  }
   // ---- epilogue: accumulators -> bf16 -> LDS (slots 0-3 hold 64 output rows each, 512 B per row, 16-byte
   // chunk c of row R at slot c ^ (R & 31)) -> full 512-byte rows to global memory. -----------------------------
   __syncthreads();
-  int le = lane;
-  asm volatile("" : "+v"(le));               // (nothing that only the epilogue needs stays live through the loop)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     // lane l holds token (l % 16) of block i, features 4 (l / 16) .. + 3 of each feature block
@@ -1357,7 +1453,7 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
   __syncthreads();
   constexpr int RPI = NT / 32;              // output rows per iteration
   uint16_t* out = P.out;
-  if (P.n_tiles > P.tiles_m * P.tiles_n) {  // (found again rather than kept: the loop has no scalar register to spare)
+  if (!HEAD && P.n_tiles > P.tiles_m * P.tiles_n) {  // (found again rather than kept: the loop has no scalar register to spare)
     int b = blockIdx.x;
     asm volatile("" : "+s"(b));
     const int n = SPLIT ? P.n_direct : P.n_tiles;
@@ -1369,8 +1465,8 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
     const int R = (tid >> 5) + it * RPI, c = tid & 31;
     const u32x4 v = *reinterpret_cast<const u32x4*>(obuf + (R & 63) * 512 + ((c ^ (R & 31)) << 4));
     if (R < rows_valid && col0 + c * 8 < P.N) {
-      const int64_t orow = P.out_index ? P.out_index[row0 + R] : row0 + R;
-      *reinterpret_cast<u32x4*>(out + orow * P.N + col0 + c * 8) = v;
+      const int64_t orow = HEAD != kHeadLogits && P.out_index ? P.out_index[row0 + R] : row0 + R;
+      *reinterpret_cast<u32x4*>(out + orow * ln_ + col0 + c * 8) = v;
     }
   }
 }
@@ -1441,6 +1537,60 @@ void launch_seg_gemm(bool w_is_kn, const TileDev* tiles, const uint16_t* act, co
     else         { if (tail) TLORA_GEMM_LAUNCH(false, true, false); else TLORA_GEMM_LAUNCH(false, false, false); }
   }
 #undef TLORA_GEMM_LAUNCH
+}
+
+// dH rows of a piece whose tiles were cut: the shares in order, scaled, as gemm_reduce_kernel
+__global__ void __launch_bounds__(256) head_reduce_kernel(const float* __restrict__ part, HeadParams head, uint16_t* __restrict__ out,
+                                                          const int32_t* __restrict__ out_index, int N, int tiles_n, int steps) {
+  const HeadShape h = head_shape(head, true, tiles_n, steps);
+  const int n_tail = h.tiles_m * tiles_n - h.split.n_direct;
+  if ((int)blockIdx.x >= n_tail) return;
+  int tm, tn;
+  gemm_tile_of(h.split.n_direct + (int)blockIdx.x, h.tiles_m, tiles_n, tm, tn);
+  const int R = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), c = (int)(threadIdx.x & 31) * 8;
+  const int t = tm * kGemmBM + R, col = tn * kGemmBN + c;
+  if (t >= h.rows || col >= N) return;
+  const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
+  const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
+  f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+  for (int k = 0; k < h.split.splits; ++k, src += stride) {
+    a += *reinterpret_cast<const f32x4*>(src);
+    b += *reinterpret_cast<const f32x4*>(src + 4);
+  }
+  const float f = head.factor[t];
+  if (f == 0.f) a = b = f32x4{0, 0, 0, 0};
+  a *= f;  b *= f;
+  *reinterpret_cast<u32x4*>(out + (int64_t)out_index[t] * N + col) =
+      u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+}
+
+void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, hipStream_t st) {
+  GemmParams P = {};
+  P.head = head;
+  P.head.kext = 0;
+  P.act = H;  P.W = W;  P.out = E;
+  P.K = d;  P.N = (head.vocab + 7) / 8 * 8;
+  P.tiles_n = head.col_tiles;
+  const dim3 grid((head.max_rows + kGemmBM - 1) / kGemmBM * P.tiles_n);
+  if (d % kGemmBK) hipLaunchKernelGGL((seg_gemm_kernel<true, true, false, false, kHeadLogits>), grid, dim3(512), 0, st, P);
+  else             hipLaunchKernelGGL((seg_gemm_kernel<true, false, false, false, kHeadLogits>), grid, dim3(512), 0, st, P);
+}
+
+void launch_head_grad(const HeadParams& head, const uint16_t* E, const uint16_t* E_tail, const uint16_t* W, const uint16_t* W_tail,
+                      uint16_t* dH, const int32_t* out_index, int d, float* part, hipStream_t st) {
+  GemmParams P = {};
+  P.head = head;
+  P.act = E;  P.W = W;  P.Sx = E_tail;  P.packed = W_tail;  P.out = dH;  P.out_index = out_index;
+  P.K = head.vocab / kGemmBK * kGemmBK;  P.N = d;  P.ra = kGemmBK;
+  P.head.kext = head.vocab % kGemmBK ? kGemmBK : 0;
+  P.tiles_n = (d + kGemmBN - 1) / kGemmBN;
+  P.part = part;  P.part_rows = kGemmBM;
+  // as many workgroups as the most that any number of rows asks for: whole rounds, and one of shares
+  const int tiles = (head.max_rows + kGemmBM - 1) / kGemmBM * P.tiles_n;
+  const int cut = std::min(tiles, 255);
+  hipLaunchKernelGGL((seg_gemm_kernel<false, false, false, true, kHeadGrad>), dim3(tiles / 256 * 256 + 256), dim3(512), 0, st, P);
+  hipLaunchKernelGGL(head_reduce_kernel, dim3(cut, kGemmBM / 8), dim3(256), 0, st, part, P.head, dH, out_index, d, P.tiles_n,
+                     (P.K + P.head.kext) / kGemmBK);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -2364,44 +2514,6 @@ void launch_adamw(const AdamwDev* tensors, int count, int64_t max_n, hipStream_t
 // Glue of the MLP block around the three fused projections: RMSNorm, gated SiLU, residual.  All HBM-bound,
 // 16-byte accesses, fp32 arithmetic; BF = tensors are bf16 (else fp32).  8 elements per lane and access.
 // ---------------------------------------------------------------------------------------------------
-template <bool BF>
-__device__ __forceinline__ void load8(const void* p, int64_t i, float (&v)[8]) {
-  if (BF) {
-    const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[2 * e] = __builtin_bit_cast(float, r[e] << 16);
-      v[2 * e + 1] = __builtin_bit_cast(float, r[e] & 0xffff0000u);
-    }
-  } else {
-    const f32x4* f = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-    const f32x4 a = f[0], b = f[1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = a[e];  v[4 + e] = b[e]; }
-  }
-}
-template <bool BF>
-__device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[8]) {
-  if (BF) {
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + i) =
-        u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-  } else {
-    f32x4* f = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
-    f[0] = f32x4{v[0], v[1], v[2], v[3]};
-    f[1] = f32x4{v[4], v[5], v[6], v[7]};
-  }
-}
-// sum over the 256 threads of a workgroup (every thread gets the total)
-__device__ __forceinline__ float block_sum(float x, float* red) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  const float t = red[0] + red[1] + red[2] + red[3];
-  __syncthreads();
-  return t;
-}
-
 // Xn[t, :] = X[t, :] * rstd_t * gamma,  rstd_t = 1 / sqrt(mean(X[t, :]^2) + eps).  One workgroup per row.
 // CH: the row is kept in registers between the sum and the result, CH chunks of 8 per thread (rows of up to 2048 CH features;
 // loads past the row repeat its last chunk and are not used).  CH = 0: any width, the row is read twice.  A CU's eight

@@ -1,0 +1,594 @@
+// gfx950 kernels of a training step around the decoder layers: what the vocabulary projection's cross entropy does beside its two
+// matrix products, the residual stream and norms between two blocks, and activations in 8 bits.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "tlora_device.h"
+#include "tlora_kernels.h"
+
+namespace tlora {
+namespace {
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+// sum over the 1024 threads of a workgroup, every thread gets it; the order is fixed
+__device__ __forceinline__ double block_sum_1024(double x, double* red) {
+  x = wave_sum(x);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double t = 0.0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) t += red[w];
+  __syncthreads();
+  return t;
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Cross entropy.  Workgroup 0 lists the tokens that have a loss, in token order; workgroup 1 + j sums job j's weights and notes
+// what each of its tokens' losses counts for (dloss, or weight / sum).  Tokens without a loss get zeros.
+// ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ bool ce_live(int y, int vocab) { return (unsigned)y < (unsigned)vocab; }
+
+__global__ void __launch_bounds__(1024) ce_prepare_kernel(CeTokens c, const float* __restrict__ dloss, float* __restrict__ loss,
+                                                          float* __restrict__ lse) {
+  __shared__ double red[16];
+  __shared__ int counts[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x == 0) {
+    int base = 0;
+    for (int t0 = 0; t0 < c.T; t0 += 8192) {          // eight neighbouring tokens per thread
+      int y[8], n = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int t = t0 + tid * 8 + k;
+        y[k] = t < c.T ? c.targets[t] : -1;
+        n += ce_live(y[k], c.vocab) ? 1 : 0;
+      }
+      int before = n;                                  // tokens up to this thread's last, inside its wave
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(before, o, 64);
+        if (lane >= o) before += v;
+      }
+      if (lane == 63) counts[wave] = before;
+      __syncthreads();
+      int at = base + before - n, all = 0;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        if (w < wave) at += counts[w];
+        all += counts[w];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (ce_live(y[k], c.vocab)) {
+          c.list[at] = t0 + tid * 8 + k;
+          c.target[at] = y[k];
+          ++at;
+        }
+      base += all;
+      __syncthreads();
+    }
+    if (tid == 0) *c.live = base;
+    return;
+  }
+  const int j = (int)blockIdx.x - 1;
+  const int a = (int)c.offsets[j], b = (int)c.offsets[j + 1];
+  const bool grad = c.share != nullptr;
+  double w = 0.0;
+  for (int t = a + tid; t < b; t += 1024) {
+    const bool on = ce_live(c.targets[t], c.vocab);
+    if (on) w += c.weights ? (double)c.weights[t] : 1.0;
+    else {
+      if (loss) loss[t] = 0.f;
+      if (lse) lse[t] = 0.f;
+    }
+  }
+  if (!grad) return;
+  const double total = block_sum_1024(w, red);
+  for (int t = a + tid; t < b; t += 1024) {
+    float g = 0.f;
+    if (ce_live(c.targets[t], c.vocab)) {
+      if (dloss) g = dloss[t];
+      else if (total != 0.0) g = (float)((c.weights ? (double)c.weights[t] : 1.0) / total);
+    }
+    c.share[t] = g;
+  }
+}
+
+// job_loss_j = sum w loss / sum w
+__global__ void __launch_bounds__(1024) ce_jobs_kernel(CeTokens c, float* __restrict__ job_loss) {
+  __shared__ double red[16];
+  const int a = (int)c.offsets[blockIdx.x], b = (int)c.offsets[blockIdx.x + 1];
+  double w = 0.0, s = 0.0;
+  for (int t = a + (int)threadIdx.x; t < b; t += 1024)
+    if (ce_live(c.targets[t], c.vocab)) {
+      const double v = c.weights ? (double)c.weights[t] : 1.0;
+      w += v;
+      s += v * (double)c.token_loss[t];
+    }
+  w = block_sum_1024(w, red);
+  s = block_sum_1024(s, red);
+  if (threadIdx.x == 0) job_loss[blockIdx.x] = w != 0.0 ? (float)(s / w) : 0.f;
+}
+
+// The rows of a piece's tokens side by side: a wave per row of row_bytes (a multiple of 16).
+__global__ void __launch_bounds__(256) ce_gather_kernel(const int32_t* __restrict__ live, int first, int max_rows,
+                                                        const int32_t* __restrict__ list, const uint8_t* __restrict__ src,
+                                                        uint8_t* __restrict__ dst, int64_t row_bytes) {
+  const int r = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+  if (r >= min(*live - first, max_rows)) return;
+  const u32x4* const s = reinterpret_cast<const u32x4*>(src + (int64_t)list[first + r] * row_bytes);
+  u32x4* const d = reinterpret_cast<u32x4*>(dst + (int64_t)r * row_bytes);
+  for (int64_t i = threadIdx.x & 63; i < row_bytes / 16; i += 64) d[i] = s[i];
+}
+
+// dH rows of tokens without a loss
+__global__ void __launch_bounds__(256) ce_zero_rows_kernel(const int32_t* __restrict__ targets, int T, int vocab,
+                                                           uint8_t* __restrict__ dst, int64_t row_bytes) {
+  const int t = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+  if (t >= T || ce_live(targets[t], vocab)) return;
+  u32x4* const d = reinterpret_cast<u32x4*>(dst + (int64_t)t * row_bytes);
+  for (int64_t i = threadIdx.x & 63; i < row_bytes / 16; i += 64) d[i] = u32x4{0, 0, 0, 0};
+}
+
+// The last vocab % 32 columns of W as rows of 32, zeros behind them.
+__global__ void __launch_bounds__(256) ce_tail_kernel(const uint16_t* __restrict__ W, int64_t ld, int d, int vocab,
+                                                      uint16_t* __restrict__ tail) {
+  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x, n = i >> 5, c = i & 31, v = vocab / 32 * 32 + c;
+  if (n < d) tail[i] = v < vocab ? W[(int64_t)n * ld + v] : (uint16_t)0;
+}
+
+// A row's statistics become its logarithm of the sum and its loss; with GRAD its exponentials become those of the gradient: all
+// relative to one reference rho, the target's less the sum itself, and factor = share * exp(rho - lse).  rho is 0 unless the sum
+// itself is out of range for it, so that as a rule (logits within head_reference's bounds) one element of the row is touched; a
+// tile that took a reference of its own is scaled.  A wave per row.
+template <bool GRAD>
+__global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c, uint16_t* __restrict__ E, uint16_t* __restrict__ E_tail,
+                                                        float* __restrict__ factor, float* __restrict__ loss, float* __restrict__ lse) {
+  const int r = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (r >= min(*h.live - h.first, h.max_rows)) return;
+  const int t = c.list[h.first + r];
+  const HeadStat* const st = h.stats + (int64_t)r * h.col_tiles;
+  float sum = 0.f;
+  bool plain = true;
+  for (int i = lane; i < h.col_tiles; i += 64) {
+    const HeadStat s = st[i];
+    plain = plain && s.ref == 0.f;
+    sum += s.sum;
+  }
+  plain = __all(plain);
+  float l;
+  if (plain) {
+    l = logf(wave_sum(sum));
+  } else {
+    float top = -__builtin_huge_valf();
+    for (int i = lane; i < h.col_tiles; i += 64) top = fmaxf(top, st[i].ref + logf(st[i].sum));
+    top = wave_max(top);
+    if (!(fabsf(top) < __builtin_huge_valf())) top = 0.f;
+    float s = 0.f;
+    for (int i = lane; i < h.col_tiles; i += 64) s += st[i].sum * expf(st[i].ref - top);
+    l = top + logf(wave_sum(s));
+  }
+  const float zy = h.target_logit[r];
+  if (lane == 0) {
+    const float v = l - zy;
+    c.token_loss[t] = v;
+    if (loss) loss[t] = v;
+    if (lse) lse[t] = l;
+  }
+  if (!GRAD) return;
+  const float rho = l >= -20.f && l <= 80.f ? 0.f : l;
+  uint16_t* const row = E + (int64_t)r * h.ld;
+  const int n8 = (h.vocab + 7) & ~7;
+  if (!plain || rho != 0.f)
+    for (int i = 0; i < h.col_tiles; ++i) {
+      const float ref = st[i].ref;
+      if (ref == rho) continue;
+      const float f = expf(ref - rho);
+      const int col = i * kGemmBN + lane * 4;
+      if (col < n8) {
+        u32x2* const p = reinterpret_cast<u32x2*>(row + col);
+        const u32x2 v = *p;
+        u32x2 o;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          o[e] = pack_bf16x2(__builtin_bit_cast(float, v[e] << 16) * f, __builtin_bit_cast(float, v[e] & 0xffff0000u) * f);
+        *p = o;
+      }
+    }
+  const int y = h.target[r];
+  const uint16_t at_y = (uint16_t)(pack_bf16x2(expf(l - rho) * expm1f(zy - l), 0.f) & 0xffffu);
+  __threadfence_block();                               // (the tail reads what other lanes may have scaled)
+  const int k0 = h.vocab & ~31, rest = h.vocab - k0;
+  if (rest && lane < 32) {
+    uint16_t v = lane < rest ? row[k0 + lane] : (uint16_t)0;
+    if (k0 + lane == y) v = at_y;
+    E_tail[(int64_t)r * 32 + lane] = v;
+  }
+  if (lane == 0) {
+    row[y] = at_y;
+    factor[r] = c.share[t] * expf(rho - l);
+  }
+}
+
+}  // namespace
+
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const float* dloss, float* loss, float* lse, hipStream_t st) {
+  hipLaunchKernelGGL(ce_prepare_kernel, dim3(1 + num_jobs), dim3(1024), 0, st, c, dloss, loss, lse);
+}
+void launch_ce_jobs(const CeTokens& c, int num_jobs, float* job_loss, hipStream_t st) {
+  hipLaunchKernelGGL(ce_jobs_kernel, dim3(num_jobs), dim3(1024), 0, st, c, job_loss);
+}
+void launch_ce_gather(const HeadParams& h, const CeTokens& c, const uint16_t* H, uint16_t* rows, int d, hipStream_t st) {
+  hipLaunchKernelGGL(ce_gather_kernel, dim3((h.max_rows + 3) / 4), dim3(256), 0, st, h.live, h.first, h.max_rows, c.list,
+                     reinterpret_cast<const uint8_t*>(H), reinterpret_cast<uint8_t*>(rows), (int64_t)d * 2);
+}
+void launch_ce_zero_rows(const CeTokens& c, uint16_t* dH, int d, hipStream_t st) {
+  if (c.T == 0) return;
+  hipLaunchKernelGGL(ce_zero_rows_kernel, dim3((c.T + 3) / 4), dim3(256), 0, st, c.targets, c.T, c.vocab,
+                     reinterpret_cast<uint8_t*>(dH), (int64_t)d * 2);
+}
+void launch_ce_tail(const uint16_t* W, int64_t ld, int d, int vocab, uint16_t* tail, hipStream_t st) {
+  hipLaunchKernelGGL(ce_tail_kernel, dim3((d * 32 + 255) / 256), dim3(256), 0, st, W, ld, d, vocab, tail);
+}
+void launch_ce_finish(const HeadParams& h, const CeTokens& c, uint16_t* E, uint16_t* E_tail, float* factor, float* loss, float* lse,
+                      hipStream_t st) {
+  const dim3 grid((h.max_rows + 3) / 4);
+  if (E) hipLaunchKernelGGL(ce_finish_kernel<true>, grid, dim3(256), 0, st, h, c, E, E_tail, factor, loss, lse);
+  else   hipLaunchKernelGGL(ce_finish_kernel<false>, grid, dim3(256), 0, st, h, c, E, E_tail, factor, loss, lse);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Residual stream and norms between two blocks (see include/tlora.h).  fp32 arithmetic on the inputs as they are; every result is
+// rounded once.  A launch has the jobs of one group as an argument, a workgroup finds its job by bisection.
+// ---------------------------------------------------------------------------------------------------
+namespace {
+
+__device__ __forceinline__ int norm_job(const NormJobs& jobs, int unit) {
+  int lo = 0, hi = jobs.n - 1;                          // the last job whose first unit is not beyond `unit`
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (jobs.job[mid].unit0 <= unit) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+template <bool BF>
+__device__ __forceinline__ void load8_or(const void* p, int64_t i, float other, float (&v)[8]) {
+  if (p) {
+    load8<BF>(p, i, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = other;
+  }
+}
+
+// units are rows
+template <bool BF>
+__global__ void __launch_bounds__(256) norm_fwd_kernel(NormArgs a, NormJobs jobs, void* __restrict__ H, void* __restrict__ Xn) {
+  __shared__ float red[4];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int64_t row = (int64_t)(jb.row0 + (int)blockIdx.x - jb.unit0) * a.d;
+  float ss = 0.f;
+  if (a.gamma_post)
+    for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+      float y[8];
+      load8<BF>(a.Y, row + c, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
+    }
+  const float r1 = a.gamma_post ? 1.0f / sqrtf(block_sum(ss, red) / (float)a.d + a.eps) : 1.0f;
+  auto stream = [&](int c, float (&h)[8]) {
+    float y[8], g[8], p[8];
+    load8<BF>(a.Y, row + c, y);
+    load8_or<BF>(a.gamma_post, c, 1.f, p);
+    load8_or<BF>(jb.gate, c, 1.f, g);
+    load8_or<BF>(a.X, row + c, 0.f, h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] += a.res_scale * (g[e] * (y[e] * r1 * p[e]));
+  };
+  ss = 0.f;
+  if (Xn)
+    for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+      float h[8];
+      stream(c, h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += h[e] * h[e];
+    }
+  const float r2 = Xn ? 1.0f / sqrtf(block_sum(ss, red) / (float)a.d + a.eps) : 0.f;
+  for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+    float h[8];
+    stream(c, h);
+    if (H) store8<BF>(H, row + c, h);
+    if (Xn) {
+      float g[8];
+      load8<BF>(a.gamma_pre, c, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = h[e] * r2 * g[e];
+      store8<BF>(Xn, row + c, h);
+    }
+  }
+}
+
+// rstd of Y and of H, and the factor of H in D = dH + r2 (dXn gamma_pre) - H k2
+struct NormRow {
+  float r1, r2, k2, pad;
+};
+
+template <bool BF>
+__device__ __forceinline__ void norm_elements(const NormArgs& a, const void* gate, const NormGrads& g, int64_t row, int c, float r1, float r2,
+                                              float k2, float (&y)[8], float (&pn)[8], float (&h)[8], float (&gn)[8], float (&D)[8],
+                                              float (&ag)[8]) {
+  float p[8];
+  load8<BF>(a.Y, row + c, y);
+  load8_or<BF>(a.gamma_post, c, 1.f, p);
+  load8_or<BF>(gate, c, 1.f, ag);
+  load8_or<BF>(a.X, row + c, 0.f, h);
+  load8_or<BF>(g.dH, row + c, 0.f, D);
+  load8_or<BF>(g.dXn, row + c, 0.f, gn);
+  float q[8];
+  load8_or<BF>(a.gamma_pre, c, 0.f, q);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    pn[e] = p[e];
+    ag[e] *= a.res_scale;
+    h[e] += ag[e] * (y[e] * r1 * p[e]);
+    D[e] += r2 * (gn[e] * q[e]) - h[e] * k2;
+  }
+}
+
+// units are rows
+template <bool BF>
+__global__ void __launch_bounds__(256) norm_bwd_rows_kernel(NormArgs a, NormJobs jobs, NormGrads g, NormRow* __restrict__ rows) {
+  __shared__ float red[4];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int t = jb.row0 + (int)blockIdx.x - jb.unit0;
+  const int64_t row = (int64_t)t * a.d;
+  const float inv_d = 1.0f / (float)a.d;
+  float r1 = 1.f, r2 = 0.f, k2 = 0.f;
+  if (a.gamma_post) {
+    float ss = 0.f;
+    for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+      float y[8];
+      load8<BF>(a.Y, row + c, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
+    }
+    r1 = 1.0f / sqrtf(block_sum(ss, red) * inv_d + a.eps);
+  }
+  float y[8], p[8], h[8], gn[8], D[8], ag[8];
+  if (g.dXn) {
+    float ss = 0.f, dot = 0.f;
+    for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+      norm_elements<BF>(a, jb.gate, g, row, c, r1, 0.f, 0.f, y, p, h, gn, D, ag);
+      float q[8];
+      load8<BF>(a.gamma_pre, c, q);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss += h[e] * h[e];
+        dot += gn[e] * q[e] * h[e];
+      }
+    }
+    r2 = 1.0f / sqrtf(block_sum(ss, red) * inv_d + a.eps);
+    k2 = block_sum(dot, red) * r2 * r2 * r2 * inv_d;
+  }
+  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, k2, 0.f};
+  float k1 = 0.f;
+  if (a.gamma_post && g.dY) {
+    float dot = 0.f;
+    for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+      norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, k2, y, p, h, gn, D, ag);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot += ag[e] * D[e] * p[e] * y[e];
+    }
+    k1 = block_sum(dot, red) * r1 * r1 * r1 * inv_d;
+  }
+  if (!g.dX && !g.dY) return;
+  for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
+    norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, k2, y, p, h, gn, D, ag);
+    if (g.dX) store8<BF>(g.dX, row + c, D);
+    if (g.dY) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D[e] = r1 * (ag[e] * D[e] * p[e]) - y[e] * k1;
+      store8<BF>(g.dY, row + c, D);
+    }
+  }
+}
+
+// Column sums of a unit's rows: a workgroup has 512 columns, its four waves every fourth row.  partial [unit][3][d]: dgamma_post,
+// dgamma_pre, dgate.
+template <bool BF>
+__global__ void __launch_bounds__(256) norm_bwd_cols_kernel(NormArgs a, NormJobs jobs, NormGrads g, const NormRow* __restrict__ rows,
+                                                            int unit_rows, float* __restrict__ partial) {
+  __shared__ float red[4][3][512];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int t0 = jb.row0 + ((int)blockIdx.x - jb.unit0) * unit_rows, t1 = min(t0 + unit_rows, jb.row1);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.y * 512 + lane * 8;
+  float s[3][8] = {};
+  if (c < a.d)
+    for (int t = t0 + wave; t < t1; t += 4) {
+      const NormRow r = rows[t];
+      float y[8], p[8], h[8], gn[8], D[8], ag[8];
+      norm_elements<BF>(a, jb.gate, g, (int64_t)t * a.d, c, r.r1, r.r2, r.k2, y, p, h, gn, D, ag);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float yn = y[e] * r.r1;
+        s[0][e] += ag[e] * D[e] * yn;
+        s[1][e] += gn[e] * (h[e] * r.r2);
+        s[2][e] += a.res_scale * (D[e] * (yn * p[e]));
+      }
+    }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[wave][k][lane * 8 + e] = s[k][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 3 * 512; i += 256) {
+    const int k = i >> 9, x = i & 511, col = (int)blockIdx.y * 512 + x;
+    if (col < a.d)
+      partial[((int64_t)(jobs.unit_base + (int)blockIdx.x) * 3 + k) * a.d + col] =
+          (red[0][k][x] + red[1][k][x]) + (red[2][k][x] + red[3][k][x]);
+  }
+}
+
+// Sums over units in a fixed order: 64 columns per workgroup, 16 slices of the units side by side.  Vectors 0 and 1 are the gammas', over all
+// units; vector 2 + j the gate of the group's job j.
+__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* __restrict__ partial, NormJobs jobs, int first_vector, int d,
+                                                           float* gamma_post, float* gamma_pre, int all_units, int accumulate) {
+  __shared__ float red[16][64];
+  const int vec = (int)blockIdx.y + first_vector, x = threadIdx.x & 63, slice = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + x;
+  int u0 = 0, u1 = all_units, k = vec;
+  float* out = vec == 0 ? gamma_post : gamma_pre;
+  if (vec >= 2) {
+    const NormJob& jb = jobs.job[vec - 2];
+    out = jb.dgate;
+    u0 = jobs.unit_base + jb.unit0;
+    u1 = u0 + jb.units;
+    k = 2;
+  }
+  if (!out) return;
+  const int per = (u1 - u0 + 15) / 16, a = u0 + slice * per, b = min(a + per, u1);
+  float s = 0.f;
+  if (c < d)
+    for (int u = a; u < b; ++u) s += partial[((int64_t)u * 3 + k) * d + c];
+  red[slice][x] = s;
+  __syncthreads();
+  if (slice == 0 && c < d) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += red[i][x];
+    out[c] = accumulate ? out[c] + s : s;
+  }
+}
+
+}  // namespace
+
+void launch_norm_fwd(bool bf16, const NormArgs& a, const NormJobs& jobs, int rows, void* H, void* Xn, hipStream_t st) {
+  if (rows == 0) return;
+  if (bf16) hipLaunchKernelGGL(norm_fwd_kernel<true>, dim3(rows), dim3(256), 0, st, a, jobs, H, Xn);
+  else      hipLaunchKernelGGL(norm_fwd_kernel<false>, dim3(rows), dim3(256), 0, st, a, jobs, H, Xn);
+}
+void launch_norm_bwd_rows(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int rows, float* row_stats,
+                          hipStream_t st) {
+  if (rows == 0) return;
+  NormRow* const r = reinterpret_cast<NormRow*>(row_stats);
+  if (bf16) hipLaunchKernelGGL(norm_bwd_rows_kernel<true>, dim3(rows), dim3(256), 0, st, a, jobs, g, r);
+  else      hipLaunchKernelGGL(norm_bwd_rows_kernel<false>, dim3(rows), dim3(256), 0, st, a, jobs, g, r);
+}
+void launch_norm_bwd_cols(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int units, int unit_rows,
+                          const float* row_stats, float* partial, hipStream_t st) {
+  if (units == 0) return;
+  const dim3 grid(units, (a.d + 511) / 512);
+  const NormRow* const r = reinterpret_cast<const NormRow*>(row_stats);
+  if (bf16) hipLaunchKernelGGL(norm_bwd_cols_kernel<true>, grid, dim3(256), 0, st, a, jobs, g, r, unit_rows, partial);
+  else      hipLaunchKernelGGL(norm_bwd_cols_kernel<false>, grid, dim3(256), 0, st, a, jobs, g, r, unit_rows, partial);
+}
+void launch_norm_reduce(const float* partial, const NormJobs& jobs, int first_vector, int vectors, int d, float* gamma_post,
+                        float* gamma_pre, int all_units, bool accumulate, hipStream_t st) {
+  if (vectors <= 0) return;
+  hipLaunchKernelGGL(norm_reduce_kernel, dim3((d + 63) / 64, vectors), dim3(1024), 0, st, partial, jobs, first_vector, d, gamma_post,
+                     gamma_pre, all_units, accumulate ? 1 : 0);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Activations in 8 bits: 16 lanes of 8 values have a group of 128.  Bound by memory.
+// ---------------------------------------------------------------------------------------------------
+namespace {
+
+// Where a thread's values lie: row, group of the row, first column; the workgroup has 16 consecutive groups.
+struct CkptPlace {
+  int64_t row, group;      // group: over all rows
+  int col;
+  bool on;
+};
+__device__ __forceinline__ CkptPlace ckpt_place(int64_t T, int d, int groups) {
+  const int64_t g0 = (int64_t)blockIdx.x * 16;
+  const int64_t r0 = g0 / groups;
+  const int g = (int)(g0 - r0 * groups) + (int)(threadIdx.x >> 4), more = g / groups;
+  CkptPlace p;
+  p.row = r0 + more;
+  p.group = g0 + (threadIdx.x >> 4);
+  p.col = (g - more * groups) * 128 + (int)(threadIdx.x & 15) * 8;
+  p.on = p.row < T && p.col < d;
+  return p;
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(256) ckpt_pack_kernel(const void* __restrict__ X, int64_t T, int d, int groups,
+                                                        uint8_t* __restrict__ codes, uint16_t* __restrict__ scales) {
+  const CkptPlace p = ckpt_place(T, d, groups);
+  float v[8] = {};
+  if (p.on) load8<BF>(X, p.row * d + p.col, v);
+  // the largest magnitude as an integer: infinities and NaN are the largest of all
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  const float amax = __builtin_bit_cast(float, top);
+  const bool finite = top < 0x7f000000u;               // below 2^127: 127 s, rounded, stays finite
+  auto up = [](float x) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) + 0xffffu) & 0xffff0000u); };
+  float s = up(amax / 127.0f);
+  if (127.0f * s < amax) s = up(s * (1.0f + 0x1p-12f));  // (127 s is exact: the quotient had been rounded down onto the grid)
+  s = fmaxf(s, 0x1p-100f);
+  const float inv = 1.0f / s;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // The fp32 quotient.  bf16: by the reciprocal and one correction, which is exact where the quotient has few bits, as at a tie; any
+    // other quotient of two numbers of 8 bits is 2^-9 or more away from a tie.
+    const float q = v[e] * inv;
+    const float c = BF ? fmaf(fmaf(-q, s, v[e]), inv, q) : v[e] / s;
+    const int code = finite ? (int)rintf(c) : 0;
+    w[e >> 2] |= ((uint32_t)code & 0xffu) << (8 * (e & 3));
+  }
+  if (p.on) *reinterpret_cast<u32x2*>(codes + p.row * d + p.col) = u32x2{w[0], w[1]};
+  if (p.row < T && (threadIdx.x & 15) == 0)
+    scales[p.group] = finite ? (uint16_t)(__builtin_bit_cast(uint32_t, s) >> 16) : (uint16_t)0x7fc0;
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(256) ckpt_unpack_kernel(const uint8_t* __restrict__ codes, const uint16_t* __restrict__ scales, int64_t T,
+                                                          int d, int groups, void* __restrict__ X) {
+  const CkptPlace p = ckpt_place(T, d, groups);
+  if (!p.on) return;
+  const u32x2 w = *reinterpret_cast<const u32x2*>(codes + p.row * d + p.col);
+  const float s = bf16_float(scales[p.group]);
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3))) * s;
+  store8<BF>(X, p.row * d + p.col, v);
+}
+
+}  // namespace
+
+void launch_ckpt_pack(bool bf16, const void* X, int64_t T, int d, uint8_t* codes, uint16_t* scales, hipStream_t st) {
+  const int groups = (d + 127) / 128;
+  if (T == 0) return;
+  const dim3 grid((unsigned)((T * groups + 15) / 16));
+  if (bf16) hipLaunchKernelGGL(ckpt_pack_kernel<true>, grid, dim3(256), 0, st, X, T, d, groups, codes, scales);
+  else      hipLaunchKernelGGL(ckpt_pack_kernel<false>, grid, dim3(256), 0, st, X, T, d, groups, codes, scales);
+}
+void launch_ckpt_unpack(bool bf16, const uint8_t* codes, const uint16_t* scales, int64_t T, int d, void* X, hipStream_t st) {
+  const int groups = (d + 127) / 128;
+  if (T == 0) return;
+  const dim3 grid((unsigned)((T * groups + 15) / 16));
+  if (bf16) hipLaunchKernelGGL(ckpt_unpack_kernel<true>, grid, dim3(256), 0, st, codes, scales, T, d, groups, X);
+  else      hipLaunchKernelGGL(ckpt_unpack_kernel<false>, grid, dim3(256), 0, st, codes, scales, T, d, groups, X);
+}
+
+}  // namespace tlora

@@ -72,6 +72,19 @@ class tlora_layer_t(ctypes.Structure):
     _fields_ = [("attn", tlora_attn_t), ("mlp", tlora_mlp_t)]
 
 
+class tlora_norm_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("num_jobs", ctypes.c_int32), ("d_model", ctypes.c_int32),
+                ("offsets", ctypes.POINTER(ctypes.c_int64)), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float),
+                ("X", ctypes.c_void_p), ("Y", ctypes.c_void_p), ("gamma_post", ctypes.c_void_p),
+                ("gamma_pre", ctypes.c_void_p), ("gates", ctypes.POINTER(ctypes.c_void_p))]
+
+
+class tlora_ce_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("num_jobs", ctypes.c_int32), ("d_model", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("ld_w", ctypes.c_int64), ("offsets", ctypes.POINTER(ctypes.c_int64)),
+                ("H", ctypes.c_void_p), ("W", ctypes.c_void_p), ("targets", ctypes.c_void_p), ("weights", ctypes.c_void_p)]
+
+
 class tlora_sched_model_t(ctypes.Structure):
     _fields_ = [("n_points", ctypes.c_int32), ("tokens", ctypes.POINTER(ctypes.c_double)),
                 ("ms", ctypes.POINTER(ctypes.c_double)), ("ms_per_token_rank", ctypes.c_double),
@@ -95,6 +108,9 @@ EXPORTS = ["tlora_workspace_bytes", "tlora_fwd", "tlora_fwd_noalloc", "tlora_bwd
            "tlora_attention_workspace_bytes", "tlora_rope", "tlora_attention_fwd", "tlora_attention_bwd",
            "tlora_attn_workspace_bytes", "tlora_attn_fwd", "tlora_attn_bwd",
            "tlora_layer_workspace_bytes", "tlora_layer_fwd", "tlora_layer_bwd",
+           "tlora_norm_workspace_bytes", "tlora_norm_fwd", "tlora_norm_bwd",
+           "tlora_ce_workspace_bytes", "tlora_ce_fwd", "tlora_ce_fwd_bwd",
+           "tlora_ckpt_bytes", "tlora_ckpt_pack", "tlora_ckpt_unpack", "tlora_ckpt_workspace_bytes", "tlora_bwd_ckpt",
            "tlora_sched_step_ms", "tlora_sched_partition", "tlora_sched_simulate",
            "tlora_indexed_workspace_bytes", "tlora_fwd_indexed", "tlora_bwd_indexed",
            "tlora_aimd_init", "tlora_aimd_update",
@@ -103,7 +119,7 @@ EXPORTS = ["tlora_workspace_bytes", "tlora_fwd", "tlora_fwd_noalloc", "tlora_bwd
            "tlora_profile", "tlora_profile_read", "tlora_profile_clock", "tlora_strerror", "tlora_last_hip_error",
            "tlora_version"]
 KERNEL_CLASSES = ["pack", "shrink", "gemm_fwd", "gemm_bwd", "rank_grad", "grad_reduce", "f32", "w_transpose", "optimizer", "glue", "permute",
-                  "attn_fwd", "attn_bwd", "rope"]
+                  "attn_fwd", "attn_bwd", "rope", "head", "loss", "norm", "ckpt"]
 
 
 def lib() -> ctypes.CDLL:
@@ -161,6 +177,29 @@ def lib() -> ctypes.CDLL:
     L.tlora_sched_partition.argtypes = [PSM, I32, PSJ, I32P, I32P]
     L.tlora_sched_simulate.restype = ctypes.c_int
     L.tlora_sched_simulate.argtypes = [PSM, I32, PSJ, I32, DP, DP, I32P, I32P, I32P, I64P, ctypes.c_int64]
+    PN, PC, I64 = ctypes.POINTER(tlora_norm_t), ctypes.POINTER(tlora_ce_t), ctypes.c_int64
+    L.tlora_norm_workspace_bytes.restype = SZ
+    L.tlora_norm_workspace_bytes.argtypes = [PN]
+    L.tlora_norm_fwd.restype = ctypes.c_int
+    L.tlora_norm_fwd.argtypes = [PN, VP, VP, VP]
+    L.tlora_norm_bwd.restype = ctypes.c_int
+    L.tlora_norm_bwd.argtypes = [PN, VP, VP, VP, VP, VP, VP, VPP, ctypes.c_int, VP, SZ, VP]
+    L.tlora_ce_workspace_bytes.restype = SZ
+    L.tlora_ce_workspace_bytes.argtypes = [PC, I32]
+    L.tlora_ce_fwd.restype = ctypes.c_int
+    L.tlora_ce_fwd.argtypes = [PC, VP, VP, VP, VP, SZ, VP]
+    L.tlora_ce_fwd_bwd.restype = ctypes.c_int
+    L.tlora_ce_fwd_bwd.argtypes = [PC, VP, VP, VP, VP, VP, VP, SZ, VP]
+    L.tlora_ckpt_bytes.restype = SZ
+    L.tlora_ckpt_bytes.argtypes = [I64, I32]
+    L.tlora_ckpt_pack.restype = ctypes.c_int
+    L.tlora_ckpt_pack.argtypes = [I32, VP, I64, I32, VP, VP]
+    L.tlora_ckpt_unpack.restype = ctypes.c_int
+    L.tlora_ckpt_unpack.argtypes = [I32, VP, I64, I32, VP, VP]
+    L.tlora_ckpt_workspace_bytes.restype = SZ
+    L.tlora_ckpt_workspace_bytes.argtypes = [P]
+    L.tlora_bwd_ckpt.restype = ctypes.c_int
+    L.tlora_bwd_ckpt.argtypes = [P, VP, VP, VP, VPP, VPP, ctypes.c_int, VP, SZ, VP]
     PL = ctypes.POINTER(tlora_layer_t)
     L.tlora_layer_workspace_bytes.restype = SZ
     L.tlora_layer_workspace_bytes.argtypes = [PL]
@@ -312,6 +351,11 @@ def tlora_bwd(prob: tlora_problem_t, dY_ptr: int, dX_ptr: int, dA_ptrs: Optional
     _check(lib().tlora_bwd(ctypes.byref(prob), ctypes.c_void_p(dY_ptr), ctypes.c_void_p(dX_ptr) if dX_ptr else None,
                            c_dA, c_dB, int(flags), ctypes.c_void_p(ws_ptr), ctypes.c_size_t(ws_bytes),
                            ctypes.c_void_p(stream)), "tlora_bwd")
+
+
+def _ptr(t):
+    """Device address of a tensor; None for no tensor or an empty one."""
+    return ctypes.c_void_p(t.data_ptr()) if t is not None and t.numel() else None
 
 
 def _grad_ptr_arrays(J, dA_ptrs, dB_ptrs):
@@ -497,6 +541,23 @@ class LayerProblem:
                   None if dA is None else [a.data_ptr() if a.numel() else 0 for a in dA],
                   None if dB is None else [b.data_ptr() if b.numel() else 0 for b in dB],
                   (TLORA_BWD_REUSE_S if reuse_S else 0) | flags, self.ws.data_ptr(), self.ws_bytes, self._stream())
+
+    def bwd_ckpt_workspace(self) -> None:
+        """Grow the workspace to what bwd_ckpt needs.  Before the fwd whose S_j bwd_ckpt is to reuse: a new one is empty."""
+        need = int(lib().tlora_ckpt_workspace_bytes(ctypes.byref(self.prob)))
+        if need == 0:
+            raise TloraError("tlora_ckpt_workspace_bytes: invalid problem")
+        if need > self.ws_bytes:
+            self.ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.X.device)
+            self.ws_bytes = need
+
+    def bwd_ckpt(self, packed, dY, dX, dA, dB, reuse_S: bool = False, flags: int = 0) -> None:
+        """bwd from the 8-bit form of X (`packed`: the bytes of Checkpoint.pack); bwd_ckpt_workspace comes first."""
+        c_dA, c_dB = _grad_ptr_arrays(len(self.ranks), None if dA is None else [a.data_ptr() if a.numel() else 0 for a in dA],
+                                      None if dB is None else [b.data_ptr() if b.numel() else 0 for b in dB])
+        _check(lib().tlora_bwd_ckpt(ctypes.byref(self.prob), _ptr(packed), _ptr(dY), _ptr(dX), c_dA, c_dB,
+                                    (TLORA_BWD_REUSE_S if reuse_S else 0) | flags, ctypes.c_void_p(self.ws.data_ptr()),
+                                    ctypes.c_size_t(self.ws_bytes), ctypes.c_void_p(self._stream())), "tlora_bwd_ckpt")
 
     def _nano_ws(self, n_nano: int, granule: int) -> None:
         """Grow the workspace if this partition needs more (the whole batch's covers every partition of it)."""
@@ -750,6 +811,94 @@ class DecoderLayer:
                                      ctypes.c_void_p(dX.data_ptr()) if self.T else None, dA, dB, int(flags),
                                      ctypes.c_void_p(self.ws.data_ptr()), ctypes.c_size_t(self.ws_bytes),
                                      ctypes.c_void_p(self._stream())), "tlora_layer_bwd")
+
+
+class ResidualNorm:
+    """Residual stream and norms between two blocks (argument marshalling for tlora_norm_fwd / tlora_norm_bwd).
+    gamma_post, gamma_pre, X, gates (a list of one [d_model] tensor or None per job) may be None, as the C call has it."""
+
+    def __init__(self, dtype: str, offsets, X, Y, gamma_pre, eps: float, gamma_post=None, gates=None, res_scale: float = 1.0):
+        import torch
+        self.torch = torch
+        self.offsets = [int(o) for o in offsets]
+        J = len(self.offsets) - 1
+        self.J, self.d = J, int(Y.shape[1])
+        self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
+        self._gates = None if gates is None else (ctypes.c_void_p * J)(*[_ptr(g) for g in gates])
+        self._keep = [X, Y, gamma_pre, gamma_post, gates]
+        self.prob = tlora_norm_t(TLORA_BF16 if dtype == "bf16" else TLORA_F32, J, self.d, self._off, float(eps), float(res_scale),
+                                 _ptr(X), _ptr(Y), _ptr(gamma_post), _ptr(gamma_pre), self._gates)
+        self.ws_bytes = int(lib().tlora_norm_workspace_bytes(ctypes.byref(self.prob)))
+        if self.ws_bytes == 0:
+            raise TloraError("tlora_norm_workspace_bytes: invalid problem")
+        self.ws = None               # (made by the first bwd: a forward has no use for it)
+
+    def _stream(self):
+        return ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream))
+
+    def fwd(self, H, Xn) -> None:
+        _check(lib().tlora_norm_fwd(ctypes.byref(self.prob), _ptr(H), _ptr(Xn), self._stream()), "tlora_norm_fwd")
+
+    def bwd(self, dH, dXn, dX, dY, dgamma_post=None, dgamma_pre=None, dgates=None, flags: int = 0) -> None:
+        if self.ws is None:
+            self.ws = self.torch.empty(self.ws_bytes, dtype=self.torch.uint8, device=self._keep[1].device)
+        g = None if dgates is None else (ctypes.c_void_p * self.J)(*[_ptr(t) for t in dgates])
+        _check(lib().tlora_norm_bwd(ctypes.byref(self.prob), _ptr(dH), _ptr(dXn), _ptr(dX), _ptr(dY), _ptr(dgamma_post),
+                                    _ptr(dgamma_pre), g, int(flags), ctypes.c_void_p(self.ws.data_ptr()),
+                                    ctypes.c_size_t(self.ws_bytes), self._stream()), "tlora_norm_bwd")
+
+
+class LossHead:
+    """Cross entropy of the vocabulary projection (argument marshalling for tlora_ce_fwd / tlora_ce_fwd_bwd; bf16).
+    H [T, d_model], W [d_model, ld_w >= vocab], targets int32 [T], weights fp32 [T] or None.  with_grad: the workspace is sized for
+    fwd_bwd."""
+
+    def __init__(self, offsets, H, W, vocab: int, targets, weights=None, with_grad: bool = True):
+        import torch
+        self.torch = torch
+        self.offsets = [int(o) for o in offsets]
+        J = len(self.offsets) - 1
+        self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
+        self._keep = [H, W, targets, weights]
+        self.prob = tlora_ce_t(TLORA_BF16, J, int(W.shape[0]), int(vocab), int(W.shape[1]), self._off, _ptr(H), _ptr(W),
+                               _ptr(targets), _ptr(weights))
+        self.ws_bytes = int(lib().tlora_ce_workspace_bytes(ctypes.byref(self.prob), int(bool(with_grad))))
+        if self.ws_bytes == 0:
+            raise TloraError("tlora_ce_workspace_bytes: invalid problem")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=W.device)
+
+    def _tail(self):
+        return (ctypes.c_void_p(self.ws.data_ptr()), ctypes.c_size_t(self.ws_bytes),
+                ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream)))
+
+    def fwd(self, loss, lse, job_loss) -> None:
+        _check(lib().tlora_ce_fwd(ctypes.byref(self.prob), _ptr(loss), _ptr(lse), _ptr(job_loss), *self._tail()), "tlora_ce_fwd")
+
+    def fwd_bwd(self, loss, lse, job_loss, dH, dloss=None) -> None:
+        _check(lib().tlora_ce_fwd_bwd(ctypes.byref(self.prob), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(job_loss), _ptr(dH),
+                                      *self._tail()), "tlora_ce_fwd_bwd")
+
+
+class Checkpoint:
+    """An activation [tokens, d] in 8 bits: `packed` are the bytes that tlora_ckpt_pack writes and LayerProblem.bwd_ckpt reads."""
+
+    def __init__(self, dtype: str, tokens: int, d: int, device):
+        import torch
+        self.torch, self.code, self.T, self.d = torch, TLORA_BF16 if dtype == "bf16" else TLORA_F32, int(tokens), int(d)
+        n = int(lib().tlora_ckpt_bytes(self.T, self.d))
+        if n == 0:
+            raise TloraError("tlora_ckpt_bytes: invalid size")
+        self.packed = torch.empty(n, dtype=torch.uint8, device=device)
+
+    def _stream(self):
+        return ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream))
+
+    def pack(self, X) -> None:
+        _check(lib().tlora_ckpt_pack(self.code, _ptr(X), self.T, self.d, _ptr(self.packed), self._stream()), "tlora_ckpt_pack")
+
+    def unpack(self, X) -> None:
+        _check(lib().tlora_ckpt_unpack(self.code, _ptr(self.packed), self.T, self.d, _ptr(X), self._stream()),
+               "tlora_ckpt_unpack")
 
 
 class Scheduler:

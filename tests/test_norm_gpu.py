@@ -1,0 +1,219 @@
+"""Residual stream and norms between two blocks against the fp64 oracle on the same inputs.
+
+Bounds: a result is rounded once (half a step: 2^-8 bf16, 2^-24 fp32) after fp32 arithmetic whose error is at most 2^-18 of the sum of
+its terms' absolute values (sums over d <= 20000 in chains of at most d / 256 + 16 links and a dozen operations per term: below 64
+roundings of 2^-24).  A column sum over T tokens adds links to its chain: T / 512 + 64 more roundings."""
+import numpy as np
+import pytest
+
+from oracle import norm_oracle as no
+from paper_2602_07263_amd import workloads as wk
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+def _draw(seed, dtype, T, d, J, post=True, pre=True, gates=True, X=True):
+    rng = np.random.default_rng(seed)
+    r = wk.round_to_bf16 if dtype == "bf16" else (lambda a: a)
+    f = lambda *s, m=0.0, k=1.0: r((m + k * rng.normal(size=s)).astype(np.float32))
+    v = dict(X=f(T, d) if X else None, Y=f(T, d, k=0.5), dH=f(T, d), dXn=f(T, d) if pre else None,
+             gamma_post=f(d, m=1.0, k=0.1) if post else None, gamma_pre=f(d, m=1.0, k=0.1) if pre else None,
+             gates=[f(d, m=1.0, k=0.1) if j != 1 else None for j in range(J)] if gates else None)
+    return v
+
+
+def _up(a, dtype):
+    import torch
+    return None if a is None else torch.from_numpy(a).to("cuda", torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+def _norm(v, dtype, off, s):
+    from paper_2602_07263_amd import tlora
+    up = lambda a: _up(a, dtype)
+    return tlora.ResidualNorm(dtype, off, up(v["X"]), up(v["Y"]), up(v["gamma_pre"]), EPS, gamma_post=up(v["gamma_post"]),
+                              gates=None if v["gates"] is None else [up(g) for g in v["gates"]], res_scale=s)
+
+
+def _near(got, ref, mag, half, what):
+    got = got.double().cpu().numpy()
+    bound = half * np.abs(ref) + 2.0 ** -18 * mag * (1 + half) + 1e-37
+    over = np.abs(got - ref) / bound
+    assert np.all(over <= 1.0), (what, over.max())
+
+
+def _nan_like(t, n=None, f32=False):
+    import torch
+    return torch.full(t.shape if n is None else (n,), float("nan"), dtype=torch.float32 if f32 else t.dtype, device="cuda")
+
+
+# dtype, d, tokens: one token, odd feature sizes, jobs without tokens, widths beyond every register variant
+CASES = [("bf16", 8, [1]), ("bf16", 4096, [5, 1, 7]), ("bf16", 1544, [33, 0, 68]), ("f32", 264, [100, 29]), ("bf16", 256, [700, 1, 0, 323]),
+         ("bf16", 8200, [9, 4]), ("f32", 4096, [17, 40]), ("bf16", 17408, [3, 6]), ("bf16", 5120, [1030, 70])]
+
+
+@pytest.mark.parametrize("post,pre,gates,X", [(1, 1, 1, 1), (0, 1, 0, 1), (1, 0, 1, 1), (0, 1, 0, 0), (1, 1, 0, 0)],
+                         ids=["all", "pre_norm", "post_norm", "norm_alone", "no_stream"])
+@pytest.mark.parametrize("dtype,d,tokens", CASES, ids=[f"{c[0]}_{c[1]}_{sum(c[2])}" for c in CASES])
+def test_forward_and_gradient_match_the_oracle(dtype, d, tokens, post, pre, gates, X):
+    import torch
+    T, J, off = sum(tokens), len(tokens), np.concatenate([[0], np.cumsum(tokens)])
+    v = _draw(T + d, dtype, T, d, J, post, pre, gates, X)
+    s, half = 0.5, 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    kw = dict(gamma_post=v["gamma_post"], gamma_pre=v["gamma_pre"], gates=v["gates"])
+    H, Xn = no.forward(v["X"], v["Y"], off, EPS, s, **kw)
+    r = no.backward(v["X"], v["Y"], off, EPS, v["dH"], v["dXn"], s, **kw)
+    n = _norm(v, dtype, off, s)
+    Y = n._keep[1]
+    gH, gXn = _nan_like(Y), _nan_like(Y) if pre else None
+    print(f"fwd {dtype} {d} {tokens}", flush=True)
+    n.fwd(gH, gXn)
+    torch.cuda.synchronize()
+    term = np.abs(v["X"]) + np.abs(H - v["X"]) if X else np.abs(H)
+    _near(gH, H, term, half, "H")
+    if pre:
+        rstd = 1 / np.sqrt((H * H).mean(axis=1, keepdims=True) + EPS)
+        _near(gXn, Xn, np.abs(v["gamma_pre"]) * rstd * (term + np.abs(H)), half, "Xn")
+    dX, dY = _nan_like(Y), _nan_like(Y)
+    dpost = _nan_like(Y, d, True) if post else None
+    dpre = _nan_like(Y, d, True) if pre else None
+    dg = [_nan_like(Y, d, True) if j != 2 else None for j in range(J)] if gates else None
+    print("bwd", flush=True)
+    n.bwd(_up(v["dH"], dtype), _up(v["dXn"], dtype), dX, dY, dgamma_post=dpost, dgamma_pre=dpre, dgates=dg)
+    torch.cuda.synchronize()
+    _near(dX, r["dX"], r["abs_dX"], half, "dX")
+    _near(dY, r["dY"], r["abs_dY"], half, "dY")
+    chain = 1 + (T / 512 + 64) / 64
+    if post:
+        _near(dpost, r["dgamma_post"], chain * r["abs_dgamma_post"], 2.0 ** -24, "dgamma_post")
+    if pre:
+        _near(dpre, r["dgamma_pre"], chain * r["abs_dgamma_pre"], 2.0 ** -24, "dgamma_pre")
+    for j, t in enumerate(dg or []):
+        if t is not None:
+            _near(t, r["dgates"][j], chain * r["abs_dgates"][j], 2.0 ** -24, f"dgate {j}")
+    # the same call without the sums, and with one gradient alone: the same bits
+    dX2, dY2 = _nan_like(Y), _nan_like(Y)
+    n.bwd(_up(v["dH"], dtype), _up(v["dXn"], dtype), dX2, dY2)
+    dY3 = _nan_like(Y)
+    n.bwd(_up(v["dH"], dtype), _up(v["dXn"], dtype), None, dY3)
+    torch.cuda.synchronize()
+    assert torch.equal(dX, dX2) and torch.equal(dY, dY2) and torch.equal(dY, dY3)
+
+
+def test_missing_upstream_gradients_are_zeros():
+    import torch
+    v = _draw(3, "bf16", 50, 512, 2)
+    off = [0, 20, 50]
+    n = _norm(v, "bf16", off, 0.7)
+    for dH, dXn in ((v["dH"], None), (None, v["dXn"])):
+        zeros = np.zeros_like(v["dH"])
+        got, ref = [], []
+        for out, a, b in ((got, dH, dXn), (ref, zeros if dH is None else dH, zeros if dXn is None else dXn)):
+            t = [_nan_like(n._keep[1]), _nan_like(n._keep[1]), _nan_like(n._keep[1], 512, True), _nan_like(n._keep[1], 512, True),
+                 _nan_like(n._keep[1], 512, True)]
+            n.bwd(_up(a, "bf16"), _up(b, "bf16"), t[0], t[1], dgamma_post=t[2], dgamma_pre=t[3], dgates=[t[4], None])
+            out += t
+        torch.cuda.synchronize()
+        for a, b in zip(got, ref):
+            assert torch.equal(a, b)
+
+
+def test_accumulate_and_jobs_without_tokens():
+    import torch
+    v = _draw(5, "bf16", 300, 264, 4)
+    off = [0, 0, 100, 100, 300]
+    n = _norm(v, "bf16", off, 1.0)
+    Y = n._keep[1]
+    new = lambda x: torch.full((264,), x, device="cuda")
+    dX, dY = _nan_like(Y), _nan_like(Y)
+    a = [new(float("nan")) for _ in range(6)]
+    n.bwd(_up(v["dH"], "bf16"), _up(v["dXn"], "bf16"), dX, dY, dgamma_post=a[0], dgamma_pre=a[1], dgates=a[2:])
+    b = [new(2.0) for _ in range(6)]
+    n.bwd(_up(v["dH"], "bf16"), _up(v["dXn"], "bf16"), dX, dY, dgamma_post=b[0], dgamma_pre=b[1], dgates=b[2:], flags=4)
+    torch.cuda.synchronize()
+    assert not a[2].any() and not a[4].any()
+    for x, y in zip(a, b):
+        assert torch.equal(x + 2.0, y)
+    empty = _norm({**v, "X": v["X"][:0], "Y": v["Y"][:0]}, "bf16", [0, 0, 0, 0, 0], 1.0)
+    empty.ws = torch.empty(empty.ws_bytes, dtype=torch.uint8, device="cuda")
+    c = [new(float("nan")) for _ in range(6)]
+    empty.fwd(None, None)
+    empty.bwd(None, None, None, None, dgamma_post=c[0], dgamma_pre=c[1], dgates=c[2:])
+    torch.cuda.synchronize()
+    assert not any(t.any() for t in c)
+
+
+def test_more_jobs_than_a_launch_takes():
+    import torch
+    rng = np.random.default_rng(6)
+    tokens = rng.integers(0, 4, 301)
+    off, T, d = np.concatenate([[0], np.cumsum(tokens)]), int(tokens.sum()), 72
+    v = _draw(7, "f32", T, d, 301)
+    n = _norm(v, "f32", off, 0.5)
+    Y = n._keep[1]
+    H, Xn = _nan_like(Y), _nan_like(Y)
+    n.fwd(H, Xn)
+    kw = dict(gamma_post=v["gamma_post"], gamma_pre=v["gamma_pre"], gates=v["gates"])
+    rH, _ = no.forward(v["X"], v["Y"], off, EPS, 0.5, **kw)
+    r = no.backward(v["X"], v["Y"], off, EPS, v["dH"], v["dXn"], 0.5, **kw)
+    dX, dY = _nan_like(Y), _nan_like(Y)
+    g = [_nan_like(Y, d, True) for _ in tokens]
+    dpost, dpre = _nan_like(Y, d, True), _nan_like(Y, d, True)
+    n.bwd(_up(v["dH"], "f32"), _up(v["dXn"], "f32"), dX, dY, dgamma_post=dpost, dgamma_pre=dpre, dgates=g)
+    torch.cuda.synchronize()
+    _near(H, rH, np.abs(v["X"]) + np.abs(rH - v["X"]), 2.0 ** -24, "H")
+    _near(dX, r["dX"], r["abs_dX"], 2.0 ** -24, "dX")
+    _near(dpost, r["dgamma_post"], 3 * r["abs_dgamma_post"], 2.0 ** -24, "dgamma_post")
+    _near(dpre, r["dgamma_pre"], 3 * r["abs_dgamma_pre"], 2.0 ** -24, "dgamma_pre")
+    for j in range(301):
+        _near(g[j], r["dgates"][j], 3 * r["abs_dgates"][j], 2.0 ** -24, j)
+
+
+def test_not_a_number_stays_in_its_row():
+    import torch
+    v = _draw(8, "bf16", 40, 256, 1)
+    off = [0, 40]
+    a = _norm(v, "bf16", off, 1.0)
+    v["Y"] = v["Y"].copy()
+    v["Y"][11, 3] = np.inf
+    b = _norm(v, "bf16", off, 1.0)
+    res = []
+    for n in (a, b):
+        t = [_nan_like(n._keep[1]) for _ in range(4)]
+        n.fwd(t[0], t[1])
+        n.bwd(_up(v["dH"], "bf16"), _up(v["dXn"], "bf16"), t[2], t[3])
+        res.append(t)
+    torch.cuda.synchronize()
+    keep = [i for i in range(40) if i != 11]
+    for x, y in zip(*res):
+        assert torch.equal(x[keep], y[keep])
+        assert not torch.isfinite(y[11]).all()
+
+
+def test_replays_from_a_captured_stream():
+    import torch
+    v = _draw(9, "bf16", 333, 1024, 3)
+    off = [0, 100, 101, 333]
+    n = _norm(v, "bf16", off, 0.5)
+    Y = n._keep[1]
+    dH, dXn = _up(v["dH"], "bf16"), _up(v["dXn"], "bf16")
+    outs = lambda: [_nan_like(Y) for _ in range(4)] + [_nan_like(Y, 1024, True) for _ in range(5)]
+
+    def call(t):
+        n.fwd(t[0], t[1])
+        n.bwd(dH, dXn, t[2], t[3], dgamma_post=t[4], dgamma_pre=t[5], dgates=t[6:])
+    ref, out = outs(), outs()
+    call(ref)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        call(out)
+    for rep in range(3):
+        for t in out:
+            t.fill_(float("nan"))
+        n.ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, ref):
+            assert torch.equal(a, b)

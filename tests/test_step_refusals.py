@@ -1,0 +1,150 @@
+"""What the operators around the decoder layers refuse, on the host, before the device is touched."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2602_07263_amd import tlora
+
+P = ctypes.c_void_p
+WS, BIG = 0x100000, 1 << 50
+
+
+def _off(tokens):
+    o = np.concatenate([[0], np.cumsum(tokens)]).astype(np.int64)
+    return (ctypes.c_int64 * len(o))(*[int(v) for v in o])
+
+
+def _ce(tokens=(5, 7), d=64, vocab=100, ld=104, dtype=tlora.TLORA_BF16, H=0x1000, W=0x2000, y=0x3000, w=None, J=None):
+    off = _off(tokens)
+    q = tlora.tlora_ce_t(dtype, len(tokens) if J is None else J, d, vocab, ld, off, P(H), P(W), P(y), P(w))
+    q._keep = off
+    return q
+
+
+def _ce_rc(q, ws=WS, n=BIG, dH=0x4000):
+    L = tlora.lib()
+    return (L.tlora_ce_fwd(ctypes.byref(q), P(0x5000), None, None, P(ws), n, None),
+            L.tlora_ce_fwd_bwd(ctypes.byref(q), None, P(0x5000), None, None, P(dH), P(ws), n, None))
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=tlora.TLORA_F32), -3), (dict(dtype=5), -3), (dict(d=60), -1), (dict(d=0), -1), (dict(vocab=0), -1), (dict(vocab=105), -1),
+    (dict(ld=103), -1), (dict(ld=(1 << 20) + 8), -1), (dict(J=0), -1), (dict(tokens=(5, -3)), -1), (dict(tokens=(1 << 25,)), -1),
+    (dict(H=0x1008), -7), (dict(W=0x2002), -7), (dict(H=0), -2), (dict(W=0), -2), (dict(y=0), -2), (dict(d=(1 << 20) + 8), -1)])
+def test_cross_entropy_refuses(kw, code):
+    q = _ce(**kw)
+    assert _ce_rc(q) == (code, code)
+    sized = tlora.lib().tlora_ce_workspace_bytes(ctypes.byref(q), 1)
+    assert (sized == 0) == (code in (-1, -3))
+
+
+def test_cross_entropy_refuses_workspaces_and_outputs():
+    L = tlora.lib()
+    q = _ce()
+    for grad in (0, 1):
+        need = L.tlora_ce_workspace_bytes(ctypes.byref(q), grad)
+        assert need > 0 and need % 256 == 0
+        assert _ce_rc(q, n=need - 1)[grad] == -4
+    assert _ce_rc(q, ws=0) == (-4, -4) and _ce_rc(q, ws=WS + 16) == (-4, -4)
+    assert _ce_rc(q, dH=0)[1] == -2 and _ce_rc(q, dH=0x4008)[1] == -7
+    assert L.tlora_ce_fwd(None, None, None, None, None, 0, None) == -2
+    assert L.tlora_ce_workspace_bytes(None, 1) == 0
+    nonzero = _ce()
+    nonzero._keep[0] = 1
+    assert _ce_rc(nonzero) == (-1, -1)
+    null = _ce()
+    null.offsets = None
+    assert _ce_rc(null) == (-2, -2)
+
+
+def test_cross_entropy_workspace_grows_with_the_tokens_and_is_bounded_by_a_piece():
+    L = tlora.lib()
+    size = lambda T, g, V=50000: L.tlora_ce_workspace_bytes(ctypes.byref(_ce((T,), 1024, V, (V + 7) // 8 * 8)), g)
+    for g in (0, 1):
+        s = [size(T, g) for T in (0, 1, 200, 300, 4000, 5000, 100000, 1 << 20)]
+        assert all(a <= b for a, b in zip(s, s[1:]))
+    # a million tokens' logits would be 105 GB
+    assert size(1 << 20, 1) < 1 << 30
+    assert size(1 << 20, 1, 1 << 20) < 3 << 30
+
+
+def _norm(tokens=(5, 7), d=64, dtype=tlora.TLORA_BF16, eps=1e-5, s=1.0, X=0x1000, Y=0x2000, post=0x3000, pre=0x4000, gates=(0x5000, 0),
+          J=None):
+    off = _off(tokens)
+    g = None if gates is None else (P * len(gates))(*[P(v) if v else None for v in gates])
+    q = tlora.tlora_norm_t(dtype, len(tokens) if J is None else J, d, off, eps, s, P(X), P(Y), P(post), P(pre), g)
+    q._keep = (off, g)
+    return q
+
+
+def _norm_rc(q, H=0x6000, Xn=0x7000, dH=0x8000, dXn=0x9000, dX=0xA000, dY=0xB000, dpost=0xC000, dpre=0xD000, dg=(0xE000, 0), flags=0,
+             ws=WS, n=BIG):
+    L = tlora.lib()
+    g = None if dg is None else (P * len(dg))(*[P(v) if v else None for v in dg])
+    return (L.tlora_norm_fwd(ctypes.byref(q), P(H), P(Xn), None),
+            L.tlora_norm_bwd(ctypes.byref(q), P(dH), P(dXn), P(dX), P(dY), P(dpost), P(dpre), g, flags, P(ws), n, None))
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=9), -3), (dict(d=12), -1), (dict(d=0), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(s=float("inf")), -1),
+    (dict(J=0), -1), (dict(tokens=(3, -1)), -1), (dict(X=0x1008), -7), (dict(Y=0x2004), -7), (dict(post=0x3002), -7), (dict(pre=0x4008), -7),
+    (dict(gates=(0x5008, 0)), -7), (dict(Y=0), -2), (dict(tokens=((1 << 24) + 1, 0)), -1)])
+def test_norm_refuses(kw, code):
+    q = _norm(**kw)
+    assert _norm_rc(q) == (code, code)
+    assert (tlora.lib().tlora_norm_workspace_bytes(ctypes.byref(q)) == 0) == (code in (-1, -3))
+
+
+def test_norm_refuses_outputs_without_their_inputs():
+    q = _norm()
+    assert _norm_rc(q, H=0, Xn=0)[0] == -2
+    assert _norm_rc(q, H=0x6008)[0] == -7 and _norm_rc(q, Xn=0x7008)[0] == -7
+    assert _norm_rc(_norm(pre=0))[0] == -2                                   # Xn without gamma_pre
+    assert _norm_rc(_norm(pre=0))[1] == -2 and _norm_rc(_norm(pre=0), dXn=0)[1] == -2     # dXn, dgamma_pre
+    assert _norm_rc(_norm(post=0))[1] == -2                                  # dgamma_post
+    assert _norm_rc(_norm(gates=None))[1] == -2                              # dgates
+    assert _norm_rc(q, dH=0, dXn=0)[1] == -2
+    assert _norm_rc(q, flags=1)[1] == -1 and _norm_rc(q, flags=2)[1] == -1
+    for k in ("dH", "dXn", "dX", "dY", "dpost", "dpre"):
+        assert _norm_rc(q, **{k: 0x8008})[1] == -7
+    assert _norm_rc(q, dg=(0xE008, 0))[1] == -7
+    assert _norm_rc(q, ws=0)[1] == -4 and _norm_rc(q, ws=WS + 128)[1] == -4
+    need = tlora.lib().tlora_norm_workspace_bytes(ctypes.byref(q))
+    assert _norm_rc(q, n=need - 1)[1] == -4
+
+
+def test_checkpoints_refuse():
+    L = tlora.lib()
+    assert L.tlora_ckpt_bytes(3, 136) == 512 + 256 and L.tlora_ckpt_bytes(0, 8) == 256
+    for T, d in ((-1, 8), (1, 12), (1, 0), (1, (1 << 20) + 8), ((1 << 24) + 1, 8)):
+        assert L.tlora_ckpt_bytes(T, d) == 0
+        assert L.tlora_ckpt_pack(1, P(0x1000), T, d, P(WS), None) == -1
+        assert L.tlora_ckpt_unpack(1, P(WS), T, d, P(0x1000), None) == -1
+    for X, packed, code in ((0, WS, -2), (0x1000, 0, -2), (0x1008, WS, -7), (0x1000, WS + 64, -7)):
+        assert L.tlora_ckpt_pack(1, P(X), 4, 8, P(packed), None) == code
+        assert L.tlora_ckpt_unpack(0, P(packed), 4, 8, P(X), None) == code
+    assert L.tlora_ckpt_pack(2, P(0x1000), 4, 8, P(WS), None) == -3
+
+
+def test_backward_from_eight_bits_refuses():
+    L = tlora.lib()
+    off = np.array([0, 10, 30], dtype=np.int64)
+    mk = lambda **k: tlora.make_problem(k.get("dtype", 1), k.get("d", 64), 128, [4, 8], off, [1.0, 1.0], 0, k.get("W", 0x2000),
+                                        [0x3000, 0x3000], [0x4000, k.get("B", 0x4000)])
+    g = (P * 2)(0x6000, 0x7000)
+    half = (P * 2)(0x6000, None)
+
+    def rc(q, packed=WS, dY=0x5000, dX=0x8000, dA=g, dB=g, flags=0, ws=WS, n=BIG):
+        return L.tlora_bwd_ckpt(ctypes.byref(q[0]), P(packed), P(dY), P(dX), dA, dB, flags, P(ws), n, None)
+    ok = mk()
+    need = L.tlora_ckpt_workspace_bytes(ctypes.byref(ok[0]))
+    assert need >= L.tlora_workspace_bytes(ctypes.byref(ok[0])) > 0
+    assert rc(ok, n=need - 1) == -4 and rc(ok, ws=0) == -4 and rc(ok, ws=WS + 32) == -4
+    assert rc(ok, packed=0) == -2 and rc(ok, packed=WS + 16) == -7
+    assert rc(ok, dY=0) == -2 and rc(ok, dY=0x5008) == -7 and rc(ok, dX=0x8008) == -7
+    assert rc(ok, dB=None) == -2 and rc(ok, dA=half) == -2
+    assert rc(ok, flags=8) == -1
+    assert rc(mk(dtype=3)) == -3 and rc(mk(d=60)) == -1 and rc(mk(W=0)) == -2 and rc(mk(B=0)) == -2
+    assert L.tlora_ckpt_workspace_bytes(ctypes.byref(mk(d=60)[0])) == 0
+    assert L.tlora_bwd_ckpt(None, P(WS), P(0x5000), None, None, None, 0, P(WS), BIG, None) == -2
