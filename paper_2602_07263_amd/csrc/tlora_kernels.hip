@@ -983,6 +983,14 @@ __device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, in
   tn = __builtin_amdgcn_readfirstlane(Lg / gsize);
 }
 
+// op over lanes l, l ^ 16, l ^ 32, l ^ 48, in registers (row swaps of the lane's value with itself).
+template <class Op>
+__device__ __forceinline__ float across_16_32(float x, const Op& op) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  x = op(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return op(__builtin_bit_cast(float, (uint32_t)h[0]), __builtin_bit_cast(float, (uint32_t)h[1]));
+}
 // What a tile of logits leaves of itself.  A lane holds tokens 16 i + l % 16 of its wave's 128 rows and features 4 (l / 16) .. + 3 of
 // each of the wave's four blocks of 16 columns.  The row's exponentials are taken relative to 0 where its largest logit in the tile
 // lies within kHeadPlain, so that the tiles of a row agree on the reference and the gradient's product can add them up as they are;
@@ -996,19 +1004,20 @@ __device__ __forceinline__ void head_softmax_tile(const HeadParams& h, f32x4 (&a
   float* const wsum = scratch + 4 * kGemmBM;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_barrier(0);         // (row after row: the tile's accumulators leave no room for more at once)
     float m = -__builtin_huge_valf();
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (c0 + j * 16 + e < h.vocab) m = fmaxf(m, acc[j][i][e]);
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    m = across_16_32(m, [](float a, float b) { return fmaxf(a, b); });
     if (lane < 16) wmax[wn * kGemmBM + wm * 128 + i * 16 + lane] = m;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_barrier(0);         // (row after row: the tile's accumulators leave no room for more at once)
     const int R = wm * 128 + i * 16 + (lane & 15);
     const float m = fmaxf(fmaxf(wmax[R], wmax[kGemmBM + R]), fmaxf(wmax[2 * kGemmBM + R], wmax[3 * kGemmBM + R]));
     const float ref = head_reference(m);
@@ -1024,8 +1033,7 @@ __device__ __forceinline__ void head_softmax_tile(const HeadParams& h, f32x4 (&a
         acc[j][i][e] = x;
         s += x;
       }
-    s += __shfl_xor(s, 16, 64);
-    s += __shfl_xor(s, 32, 64);
+    s = across_16_32(s, [](float a, float b) { return a + b; });
     if (lane < 16) wsum[wn * kGemmBM + R] = s;
     if (y >= 0 && y < 64 && (y & 15) < 4) h.target_logit[row0 + R] = zy;
   }
@@ -1232,7 +1240,18 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
         //  to one step, so base and step clamping are wave-uniform
         const int t = min(max(tq + (wave >> 2), 0), ntot - 1);
         const char* const sb = (t >= nfull ? e_base : w_base) + (int64_t)t * 64 * ln_;
-        if (t < w_plain) {
+        if (HEAD == kHeadLogits && t < w_plain) {
+          // (the same addresses, made again from the lane's number: with the softmax behind the loop the compiler kept the two
+          // offsets in scratch memory, and waiting for them there meant waiting for every load in flight: 5.2 ms instead of 3.1 for
+          // 3840 tokens, 4096 x 128000)
+          int l0 = lane;
+          asm volatile("" : "+v"(l0));
+          const uint32_t row = (uint32_t)(l0 >> 5) * (uint32_t)(ln_ * 2);
+          const uint32_t c = (uint32_t)((l0 & 31) ^ ((l0 >> 5) << 2) ^ ((wave & 1) << 1)) * 16;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            dma16s(row + (i & 1 ? c ^ 128 : c), uniform_ptr(sb + (int64_t)((wave & 3) * 8 + i * 2) * 2 * ln_), dst + i * 1024);
+        } else if (t < w_plain) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             dma16s(kn_off[i & 1], uniform_ptr(sb + (int64_t)(i >> 1) * 8 * ln_), dst + i * 1024);   // i / 2: 4 k-rows on
