@@ -2270,7 +2270,7 @@ int ce_plan(const tlora_ce_t* p, bool grad, CePlan& C) {
   size_t w = 0;
   auto place = [&](size_t bytes) { const size_t at = w;  w = align_up(w + bytes, 256);  return at; };
   const size_t T = (size_t)C.T, n = (size_t)C.piece, d = (size_t)p->d_model;
-  C.off_offsets = place(sizeof(int64_t) * ((size_t)p->num_jobs + 1));
+  C.off_offsets = place(sizeof(int32_t) * ((size_t)p->num_jobs + 1));
   C.off_live = place(sizeof(int32_t));
   C.off_list = place(sizeof(int32_t) * T);
   C.off_target = place(sizeof(int32_t) * T);
@@ -2284,8 +2284,8 @@ int ce_plan(const tlora_ce_t* p, bool grad, CePlan& C) {
     C.off_E = place(2 * n * (size_t)p->ld_w);
     C.off_E_tail = place(2 * n * 32);
     C.off_W_tail = place(2 * d * 32);
-    C.off_part = place(kHeadPartBytes);
   }
+  C.off_part = place(kHeadPartBytes);
   C.total = w;
   return TLORA_OK;
 }
@@ -2305,8 +2305,8 @@ int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, floa
   const int d = p->d_model, J = p->num_jobs;
   const uint16_t* const W = static_cast<const uint16_t*>(p->W);
   CeTokens c;
-  c.T = (int32_t)C.T;  c.vocab = p->vocab;
-  c.offsets = reinterpret_cast<const int64_t*>(ws + C.off_offsets);
+  c.T = (int32_t)C.T;  c.vocab = p->vocab;  c.d = d;
+  c.offsets = reinterpret_cast<const int32_t*>(ws + C.off_offsets);
   c.targets = p->targets;  c.weights = p->weights;
   c.live = reinterpret_cast<int32_t*>(ws + C.off_live);
   c.list = reinterpret_cast<int32_t*>(ws + C.off_list);
@@ -2317,12 +2317,19 @@ int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, floa
   uint16_t* const E_tail = reinterpret_cast<uint16_t*>(ws + C.off_E_tail);
   uint16_t* const W_tail = reinterpret_cast<uint16_t*>(ws + C.off_W_tail);
   uint16_t* const rows = reinterpret_cast<uint16_t*>(ws + C.off_rows);
+  float* const part = reinterpret_cast<float*>(ws + C.off_part);
+  const uint16_t* const H = static_cast<const uint16_t*>(p->H);
+  const bool one_piece = C.T <= kCePieceRows && C.T <= C.piece;     // (the first launch counts the list per row)
   {
     Timed t(TLORA_K_LOSS, st);
-    launch_table_write(p->offsets, sizeof(int64_t) * ((size_t)J + 1), ws + C.off_offsets, st);
-    launch_ce_prepare(c, J, dloss, loss, lse, st);
-    if (grad) launch_ce_zero_rows(c, static_cast<uint16_t*>(dH), d, st);
-    if (grad && p->vocab % 32) launch_ce_tail(W, p->ld_w, d, p->vocab, W_tail, st);
+    const std::vector<int32_t> offsets(p->offsets, p->offsets + J + 1);
+    CePrepare q;
+    q.dloss = dloss;  q.loss = loss;  q.lse = lse;
+    q.H = H;  q.dH = static_cast<uint16_t*>(dH);
+    q.rows = one_piece ? rows : nullptr;
+    q.W = W;  q.ld = p->ld_w;
+    q.W_tail = grad && p->vocab % 32 ? W_tail : nullptr;
+    launch_ce_prepare(c, J, offsets.data(), q, st);
   }
   for (int64_t first = 0; first < C.T; first += C.piece) {
     HeadParams h;
@@ -2333,25 +2340,29 @@ int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, floa
     h.stats = reinterpret_cast<HeadStat*>(ws + C.off_stats);
     float* const factor = reinterpret_cast<float*>(ws + C.off_factor);
     h.factor = factor;
-    {
+    if (!one_piece) {
       Timed t(TLORA_K_LOSS, st);
-      launch_ce_gather(h, c, static_cast<const uint16_t*>(p->H), rows, d, st);
+      launch_ce_gather(h, c, H, rows, d, st);
     }
     {
       Timed t(TLORA_K_HEAD, st);
-      launch_head_logits(h, rows, W, E, d, st);
+      launch_head_logits(h, rows, W, E, d, part, st);
     }
     {
       Timed t(TLORA_K_LOSS, st);
+      launch_head_logits_reduce(h, E, d, part, st);
       launch_ce_finish(h, c, E, E_tail, factor, loss, lse, st);
     }
     if (grad) {
-      Timed t(TLORA_K_HEAD, st);
-      launch_head_grad(h, E, E_tail, W, W_tail, static_cast<uint16_t*>(dH), c.list + first, d,
-                       reinterpret_cast<float*>(ws + C.off_part), st);
+      {
+        Timed t(TLORA_K_HEAD, st);
+        launch_head_grad(h, E, E_tail, W, W_tail, static_cast<uint16_t*>(dH), c.list + first, d, part, st);
+      }
+      Timed t(TLORA_K_LOSS, st);
+      launch_head_grad_reduce(h, c, static_cast<uint16_t*>(dH), c.list + first, d, part, J, first + C.piece < C.T ? nullptr : job_loss, st);
     }
   }
-  if (job_loss) {
+  if (job_loss && (!grad || C.T == 0)) {
     Timed t(TLORA_K_LOSS, st);
     launch_ce_jobs(c, J, job_loss, st);
   }

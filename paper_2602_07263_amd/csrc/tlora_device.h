@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "tlora_kernels.h"
+
 namespace tlora {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -54,6 +56,40 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
   const float t = red[0] + red[1] + red[2] + red[3];
   __syncthreads();
   return t;
+}
+
+// Tile L of the walk: groups of 4 row tiles, so that workgroups that run together share activation and weight panels.
+__device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, int& tm, int& tn) {
+  constexpr int GM = 4;
+  const int per_group = GM * tiles_n;
+  const int grp = L / per_group, first_m = grp * GM;
+  const int gsize = min(GM, tiles_m - first_m);
+  const int Lg = L - grp * per_group;
+  // (the divisions run on the vector ALU; everything derived from the tile id is wave-uniform and belongs in
+  // scalar registers)
+  tm = __builtin_amdgcn_readfirstlane(first_m + Lg % gsize);
+  tn = __builtin_amdgcn_readfirstlane(Lg / gsize);
+}
+
+enum { kHeadNone = 0, kHeadLogits = 1, kHeadGrad = 2 };
+struct HeadShape {
+  int rows, tiles_m;
+  GemmSplit split;
+};
+// Rows of the piece that are there, and how a product's tiles are cut along K: whole rounds of 256 tiles (the chip's CUs) as they are,
+// the rest into as many shares as fill one round, each of kHeadShare K-steps at least (a share's sums are written and read once more:
+// 0.5 MB a tile, which takes a CU about as long as 8 steps do).
+__device__ __forceinline__ HeadShape head_shape(const HeadParams& h, int tiles_n, int steps) {
+  HeadShape s;
+  s.rows = __builtin_amdgcn_readfirstlane(min(max(*h.live - h.first, 0), h.max_rows));
+  s.tiles_m = (s.rows + kGemmBM - 1) / kGemmBM;
+  const int tiles = s.tiles_m * tiles_n, rest = tiles & 255;
+  s.split.n_direct = tiles;
+  if (rest) {
+    s.split.splits = __builtin_amdgcn_readfirstlane(max(1, min(min(256 / rest, kHeadMaxSplits), steps / kHeadShare)));
+    if (s.split.splits > 1) s.split.n_direct = tiles - rest;
+  }
+  return s;
 }
 
 }  // namespace tlora

@@ -124,6 +124,7 @@ struct HeadParams {
   const float* factor = nullptr;         // [max_rows] what a row of E W^T is multiplied by
 };
 constexpr int kHeadMaxSplits = 16;
+constexpr int kHeadShare = 8;            // K-steps
 constexpr size_t kHeadPartBytes = (size_t)256 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most one round of tiles
 // Largest logit of a row in a tile up to which exp(z) needs no reference, and from which on sums of it hold their digits.
 __host__ __device__ inline float head_reference(float m) {
@@ -131,27 +132,47 @@ __host__ __device__ inline float head_reference(float m) {
   return m <= kTop && m >= kBottom ? 0.f : m == -__builtin_huge_valf() ? 0.f : m;
 }
 // E = exp(H.W - ref) as bf16 [max_rows, ld] (null: statistics alone), zero from vocab to the next multiple of 8; stats; target_logit.
-void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, hipStream_t st);
+// Tiles that are cut leave their shares in part (kHeadPartBytes), from which launch_head_logits_reduce makes the same.
+void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, float* part, hipStream_t st);
+void launch_head_logits_reduce(const HeadParams& head, uint16_t* E, int d, const float* part, hipStream_t st);
 // dH[out_index[r]] = factor[r] * (E[r] . W^T).  The columns from vocab / 32 * 32 on come from E_tail [max_rows padded to 256, 32] and
-// W_tail [d, 32] (null if there are none).  part: kHeadPartBytes.
+// W_tail [d, 32] (null if there are none).  Cut tiles as above: launch_head_grad_reduce, which also makes the job losses (null: not
+// wanted, or not with this piece).
 void launch_head_grad(const HeadParams& head, const uint16_t* E, const uint16_t* E_tail, const uint16_t* W, const uint16_t* W_tail,
                       uint16_t* dH, const int32_t* out_index, int d, float* part, hipStream_t st);
+struct CeTokens;
+void launch_head_grad_reduce(const HeadParams& head, const CeTokens& c, uint16_t* dH, const int32_t* out_index, int d, const float* part,
+                             int num_jobs, float* job_loss, hipStream_t st);
 
 // The rest of the loss.
+constexpr int kCeArgJobs = 256;          // segments of so many jobs travel as an argument of the launch
+struct CeOffsets {
+  int32_t at[kCeArgJobs + 1];
+};
 struct CeTokens {
-  int32_t T = 0, vocab = 0;
-  const int64_t* offsets = nullptr;      // [J + 1]
+  int32_t T = 0, vocab = 0, d = 0;
+  const int32_t* offsets = nullptr;      // [J + 1] on the device
   const int32_t* targets = nullptr;      // [T]
   const float* weights = nullptr;        // [T] or null: ones
   int32_t *live = nullptr, *list = nullptr, *target = nullptr;    // the list of the tokens with a loss, and their targets
   float* share = nullptr;                // [T] what a token's loss counts for; null: no gradient
   float* token_loss = nullptr;           // [T]; written for the tokens with a loss
 };
-// The list, the shares (dloss instead of them if given), zeros in loss and lse (either may be null) of the other tokens.
-void launch_ce_prepare(const CeTokens& c, int num_jobs, const float* dloss, float* loss, float* lse, hipStream_t st);
+// Whatever the first launch of a call can do: the list, the shares (dloss instead of them if given), zeros in loss and lse (either
+// may be null) and dH (null: no gradient) of the tokens without a loss, the last columns of W as W_tail (null: none), and with `rows`
+// the rows H of a batch that is one piece.  host_offsets: [J + 1], left at c.offsets; of more than kCeArgJobs jobs by launches
+// before.
+struct CePrepare {
+  const float* dloss = nullptr;
+  float *loss = nullptr, *lse = nullptr;
+  const uint16_t* H = nullptr;
+  uint16_t *dH = nullptr, *rows = nullptr;
+  const uint16_t* W = nullptr;
+  int64_t ld = 0;
+  uint16_t* W_tail = nullptr;
+};
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const int32_t* host_offsets, const CePrepare& p, hipStream_t st);
 void launch_ce_gather(const HeadParams& h, const CeTokens& c, const uint16_t* H, uint16_t* rows, int d, hipStream_t st);
-void launch_ce_zero_rows(const CeTokens& c, uint16_t* dH, int d, hipStream_t st);
-void launch_ce_tail(const uint16_t* W, int64_t ld, int d, int vocab, uint16_t* tail, hipStream_t st);
 // Statistics -> losses; E null: no gradient.
 void launch_ce_finish(const HeadParams& h, const CeTokens& c, uint16_t* E, uint16_t* E_tail, float* factor, float* loss, float* lse,
                       hipStream_t st);

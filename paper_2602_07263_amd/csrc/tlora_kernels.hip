@@ -926,26 +926,6 @@ void launch_shrink_stream(const JobDev* jobs, const TileDev* tiles, const Shrink
 // operand is fetched as a whole 128-byte line: the same bytes in half as many L2 requests (a load-only
 // replica of the two streams sustains ~15.4 TB/s this way against ~11.5 TB/s).
 // ---------------------------------------------------------------------------------------------------
-enum { kHeadNone = 0, kHeadLogits = 1, kHeadGrad = 2 };
-struct HeadShape {
-  int rows, tiles_m;
-  GemmSplit split;
-};
-// Rows of the piece that are there, and how the gradient's tiles are cut: whole rounds of 256 tiles (the chip's CUs) as they are,
-// the rest into as many shares as fill one round, each of 32 K-steps at least.
-__device__ __forceinline__ HeadShape head_shape(const HeadParams& h, bool cut, int tiles_n, int steps) {
-  HeadShape s;
-  s.rows = __builtin_amdgcn_readfirstlane(min(max(*h.live - h.first, 0), h.max_rows));
-  s.tiles_m = (s.rows + kGemmBM - 1) / kGemmBM;
-  const int tiles = s.tiles_m * tiles_n, rest = tiles & 255;
-  s.split.n_direct = tiles;
-  if (cut && rest) {
-    s.split.splits = __builtin_amdgcn_readfirstlane(max(1, min(min(256 / rest, kHeadMaxSplits), steps / 32)));
-    if (s.split.splits > 1) s.split.n_direct = tiles - rest;
-  }
-  return s;
-}
-
 struct GemmParams {
   const TileDev* tiles;
   const uint16_t* act;      // [T, K]
@@ -969,19 +949,6 @@ struct GemmParams {
   // HEAD instantiations
   HeadParams head;
 };
-
-// Tile L of the walk: groups of 4 row tiles, so that workgroups that run together share activation and weight panels.
-__device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, int& tm, int& tn) {
-  constexpr int GM = 4;
-  const int per_group = GM * tiles_n;
-  const int grp = L / per_group, first_m = grp * GM;
-  const int gsize = min(GM, tiles_m - first_m);
-  const int Lg = L - grp * per_group;
-  // (the divisions run on the vector ALU; everything derived from the tile id is wave-uniform and belongs in
-  // scalar registers)
-  tm = __builtin_amdgcn_readfirstlane(first_m + Lg % gsize);
-  tn = __builtin_amdgcn_readfirstlane(Lg / gsize);
-}
 
 // op over lanes l, l ^ 16, l ^ 32, l ^ 48, in registers (row swaps of the lane's value with itself).
 template <class Op>
@@ -1085,9 +1052,9 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
   bool cut = false, second;
   int split = 0, tail_tile = 0;
   if (HEAD) {
-    const HeadShape h = head_shape(P.head, HEAD == kHeadGrad, P.tiles_n, (P.K + P.head.kext) / 32);
+    const HeadShape h = head_shape(P.head, P.tiles_n, (P.K + P.head.kext) / 32);
     P.T = h.rows;  P.tiles_m = h.tiles_m;  P.n_tiles = h.tiles_m * P.tiles_n;
-    P.n_direct = h.split.n_direct;  P.splits = h.split.splits;
+    P.n_direct = SPLIT ? h.split.n_direct : P.n_tiles;  P.splits = SPLIT ? h.split.splits : 1;
     if ((int)blockIdx.x >= (SPLIT ? P.n_direct + (P.n_tiles - P.n_direct) * P.splits : P.n_tiles)) return;
   }
   {
@@ -1558,41 +1525,21 @@ void launch_seg_gemm(bool w_is_kn, const TileDev* tiles, const uint16_t* act, co
 #undef TLORA_GEMM_LAUNCH
 }
 
-// dH rows of a piece whose tiles were cut: the shares in order, scaled, as gemm_reduce_kernel
-__global__ void __launch_bounds__(256) head_reduce_kernel(const float* __restrict__ part, HeadParams head, uint16_t* __restrict__ out,
-                                                          const int32_t* __restrict__ out_index, int N, int tiles_n, int steps) {
-  const HeadShape h = head_shape(head, true, tiles_n, steps);
-  const int n_tail = h.tiles_m * tiles_n - h.split.n_direct;
-  if ((int)blockIdx.x >= n_tail) return;
-  int tm, tn;
-  gemm_tile_of(h.split.n_direct + (int)blockIdx.x, h.tiles_m, tiles_n, tm, tn);
-  const int R = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), c = (int)(threadIdx.x & 31) * 8;
-  const int t = tm * kGemmBM + R, col = tn * kGemmBN + c;
-  if (t >= h.rows || col >= N) return;
-  const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
-  const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
-  f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-  for (int k = 0; k < h.split.splits; ++k, src += stride) {
-    a += *reinterpret_cast<const f32x4*>(src);
-    b += *reinterpret_cast<const f32x4*>(src + 4);
-  }
-  const float f = head.factor[t];
-  if (f == 0.f) a = b = f32x4{0, 0, 0, 0};
-  a *= f;  b *= f;
-  *reinterpret_cast<u32x4*>(out + (int64_t)out_index[t] * N + col) =
-      u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+// As many workgroups as the most that any number of rows asks for: whole rounds, and one of shares.
+static dim3 head_grid(const HeadParams& head, int tiles_n) {
+  return dim3((head.max_rows + kGemmBM - 1) / kGemmBM * tiles_n / 256 * 256 + 256);
 }
-
-void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, hipStream_t st) {
+void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, float* part, hipStream_t st) {
   GemmParams P = {};
   P.head = head;
   P.head.kext = 0;
   P.act = H;  P.W = W;  P.out = E;
   P.K = d;  P.N = (head.vocab + 7) / 8 * 8;
   P.tiles_n = head.col_tiles;
-  const dim3 grid((head.max_rows + kGemmBM - 1) / kGemmBM * P.tiles_n);
+  P.part = part;  P.part_rows = kGemmBM;
+  const dim3 grid = d % kGemmBK ? dim3((head.max_rows + kGemmBM - 1) / kGemmBM * P.tiles_n) : head_grid(head, P.tiles_n);
   if (d % kGemmBK) hipLaunchKernelGGL((seg_gemm_kernel<true, true, false, false, kHeadLogits>), grid, dim3(512), 0, st, P);
-  else             hipLaunchKernelGGL((seg_gemm_kernel<true, false, false, false, kHeadLogits>), grid, dim3(512), 0, st, P);
+  else             hipLaunchKernelGGL((seg_gemm_kernel<true, false, false, true, kHeadLogits>), grid, dim3(512), 0, st, P);
 }
 
 void launch_head_grad(const HeadParams& head, const uint16_t* E, const uint16_t* E_tail, const uint16_t* W, const uint16_t* W_tail,
@@ -1604,12 +1551,7 @@ void launch_head_grad(const HeadParams& head, const uint16_t* E, const uint16_t*
   P.head.kext = head.vocab % kGemmBK ? kGemmBK : 0;
   P.tiles_n = (d + kGemmBN - 1) / kGemmBN;
   P.part = part;  P.part_rows = kGemmBM;
-  // as many workgroups as the most that any number of rows asks for: whole rounds, and one of shares
-  const int tiles = (head.max_rows + kGemmBM - 1) / kGemmBM * P.tiles_n;
-  const int cut = std::min(tiles, 255);
-  hipLaunchKernelGGL((seg_gemm_kernel<false, false, false, true, kHeadGrad>), dim3(tiles / 256 * 256 + 256), dim3(512), 0, st, P);
-  hipLaunchKernelGGL(head_reduce_kernel, dim3(cut, kGemmBM / 8), dim3(256), 0, st, part, P.head, dH, out_index, d, P.tiles_n,
-                     (P.K + P.head.kext) / kGemmBK);
+  hipLaunchKernelGGL((seg_gemm_kernel<false, false, false, true, kHeadGrad>), head_grid(head, P.tiles_n), dim3(512), 0, st, P);
 }
 
 // ---------------------------------------------------------------------------------------------------

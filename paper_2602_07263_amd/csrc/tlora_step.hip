@@ -40,16 +40,26 @@ __device__ __forceinline__ double block_sum_1024(double x, double* red) {
 
 // ---------------------------------------------------------------------------------------------------
 // Cross entropy.  Workgroup 0 lists the tokens that have a loss, in token order; workgroup 1 + j sums job j's weights and notes
-// what each of its tokens' losses counts for (dloss, or weight / sum).  Tokens without a loss get zeros.
+// what each of its tokens' losses counts for (dloss, or weight / sum).  Tokens without a loss get zeros.  Of the workgroups behind
+// those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the batch is one
+// piece moves the others' rows of H to their places, for which it counts the list up to its tokens itself (16 KB of targets at
+// most, from the L2; a launch of its own that reads the list costs 6 us); the last copy the end of W.
 // ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ bool ce_live(int y, int vocab) { return (unsigned)y < (unsigned)vocab; }
 
-__global__ void __launch_bounds__(1024) ce_prepare_kernel(CeTokens c, const float* __restrict__ dloss, float* __restrict__ loss,
-                                                          float* __restrict__ lse) {
+__device__ __forceinline__ void copy_row(const uint16_t* src, uint16_t* dst, int d, int lane) {     // src null: zeros
+  for (int i = lane * 8; i < d; i += 512)
+    *reinterpret_cast<u32x4*>(dst + i) = src ? ldg16(src + i) : u32x4{0, 0, 0, 0};
+}
+
+template <bool ARGS>
+__global__ void __launch_bounds__(1024) ce_prepare_kernel(CeTokens c, int num_jobs, int32_t* __restrict__ table, const CeOffsets offsets,
+                                                          CePrepare p, int row_groups) {
   __shared__ double red[16];
   __shared__ int counts[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x == 0) {
+    if (ARGS && tid <= num_jobs) table[tid] = offsets.at[tid];
     int base = 0;
     for (int t0 = 0; t0 < c.T; t0 += 8192) {          // eight neighbouring tokens per thread
       int y[8], n = 0;
@@ -86,71 +96,174 @@ __global__ void __launch_bounds__(1024) ce_prepare_kernel(CeTokens c, const floa
     if (tid == 0) *c.live = base;
     return;
   }
-  const int j = (int)blockIdx.x - 1;
-  const int a = (int)c.offsets[j], b = (int)c.offsets[j + 1];
-  const bool grad = c.share != nullptr;
-  double w = 0.0;
-  for (int t = a + tid; t < b; t += 1024) {
-    const bool on = ce_live(c.targets[t], c.vocab);
-    if (on) w += c.weights ? (double)c.weights[t] : 1.0;
-    else {
-      if (loss) loss[t] = 0.f;
-      if (lse) lse[t] = 0.f;
+  if ((int)blockIdx.x <= num_jobs) {
+    const int j = (int)blockIdx.x - 1;
+    const int a = ARGS ? offsets.at[j] : table[j], b = ARGS ? offsets.at[j + 1] : table[j + 1];
+    double w = 0.0;
+    for (int t = a + tid; t < b; t += 1024) {
+      const bool on = ce_live(c.targets[t], c.vocab);
+      if (on) w += c.weights ? (double)c.weights[t] : 1.0;
+      else {
+        if (p.loss) p.loss[t] = 0.f;
+        if (p.lse) p.lse[t] = 0.f;
+      }
     }
-  }
-  if (!grad) return;
-  const double total = block_sum_1024(w, red);
-  for (int t = a + tid; t < b; t += 1024) {
-    float g = 0.f;
-    if (ce_live(c.targets[t], c.vocab)) {
-      if (dloss) g = dloss[t];
-      else if (total != 0.0) g = (float)((c.weights ? (double)c.weights[t] : 1.0) / total);
+    if (!c.share) return;
+    const double total = block_sum_1024(w, red);
+    for (int t = a + tid; t < b; t += 1024) {
+      float g = 0.f;
+      if (ce_live(c.targets[t], c.vocab)) {
+        if (p.dloss) g = p.dloss[t];
+        else if (total != 0.0) g = (float)((c.weights ? (double)c.weights[t] : 1.0) / total);
+      }
+      c.share[t] = g;
     }
-    c.share[t] = g;
+    return;
   }
+  const int group = (int)blockIdx.x - 1 - num_jobs;
+  if (group < row_groups) {
+    const int t0 = group * 16, t = t0 + wave;
+    if (p.rows) {
+      int n = 0;
+      for (int i = tid; i < t0; i += 1024) n += ce_live(c.targets[i], c.vocab) ? 1 : 0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+      if (lane == 0) counts[wave] = n;
+      __syncthreads();
+    }
+    if (t >= c.T) return;
+    if (!ce_live(c.targets[t], c.vocab)) {
+      if (p.dH) copy_row(nullptr, p.dH + (int64_t)t * c.d, c.d, lane);
+    } else if (p.rows) {
+      int at = 0;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) at += counts[w] + (w < wave && ce_live(c.targets[t0 + w], c.vocab) ? 1 : 0);
+      copy_row(p.H + (int64_t)t * c.d, p.rows + (int64_t)at * c.d, c.d, lane);
+    }
+    return;
+  }
+  const int i = (group - row_groups) * 1024 + tid, n = i >> 5, v = c.vocab / 32 * 32 + (i & 31);
+  if (n < c.d) p.W_tail[i] = v < c.vocab ? p.W[(int64_t)n * p.ld + v] : (uint16_t)0;
 }
 
-// job_loss_j = sum w loss / sum w
-__global__ void __launch_bounds__(1024) ce_jobs_kernel(CeTokens c, float* __restrict__ job_loss) {
-  __shared__ double red[16];
-  const int a = (int)c.offsets[blockIdx.x], b = (int)c.offsets[blockIdx.x + 1];
+// job_loss_j = sum w loss / sum w, by the threads of a workgroup (sums: its block sum)
+template <class Sum>
+__device__ __forceinline__ void ce_job(const CeTokens& c, int j, int threads, float* job_loss, const Sum& sums) {
+  const int a = c.offsets[j], b = c.offsets[j + 1];
   double w = 0.0, s = 0.0;
-  for (int t = a + (int)threadIdx.x; t < b; t += 1024)
+  for (int t = a + (int)threadIdx.x; t < b; t += threads)
     if (ce_live(c.targets[t], c.vocab)) {
       const double v = c.weights ? (double)c.weights[t] : 1.0;
       w += v;
       s += v * (double)c.token_loss[t];
     }
-  w = block_sum_1024(w, red);
-  s = block_sum_1024(s, red);
-  if (threadIdx.x == 0) job_loss[blockIdx.x] = w != 0.0 ? (float)(s / w) : 0.f;
+  w = sums(w);
+  s = sums(s);
+  if (threadIdx.x == 0) job_loss[j] = w != 0.0 ? (float)(s / w) : 0.f;
+}
+__global__ void __launch_bounds__(1024) ce_jobs_kernel(CeTokens c, float* __restrict__ job_loss) {
+  __shared__ double red[16];
+  ce_job(c, blockIdx.x, 1024, job_loss, [&](double x) { return block_sum_1024(x, red); });
 }
 
-// The rows of a piece's tokens side by side: a wave per row of row_bytes (a multiple of 16).
+// The rows of a piece's tokens side by side: a wave per row.
 __global__ void __launch_bounds__(256) ce_gather_kernel(const int32_t* __restrict__ live, int first, int max_rows,
-                                                        const int32_t* __restrict__ list, const uint8_t* __restrict__ src,
-                                                        uint8_t* __restrict__ dst, int64_t row_bytes) {
+                                                        const int32_t* __restrict__ list, const uint16_t* __restrict__ src,
+                                                        uint16_t* __restrict__ dst, int d) {
   const int r = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
   if (r >= min(*live - first, max_rows)) return;
-  const u32x4* const s = reinterpret_cast<const u32x4*>(src + (int64_t)list[first + r] * row_bytes);
-  u32x4* const d = reinterpret_cast<u32x4*>(dst + (int64_t)r * row_bytes);
-  for (int64_t i = threadIdx.x & 63; i < row_bytes / 16; i += 64) d[i] = s[i];
+  copy_row(src + (int64_t)list[first + r] * d, dst + (int64_t)r * d, d, threadIdx.x & 63);
 }
 
-// dH rows of tokens without a loss
-__global__ void __launch_bounds__(256) ce_zero_rows_kernel(const int32_t* __restrict__ targets, int T, int vocab,
-                                                           uint8_t* __restrict__ dst, int64_t row_bytes) {
-  const int t = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
-  if (t >= T || ce_live(targets[t], vocab)) return;
-  u32x4* const d = reinterpret_cast<u32x4*>(dst + (int64_t)t * row_bytes);
-  for (int64_t i = threadIdx.x & 63; i < row_bytes / 16; i += 64) d[i] = u32x4{0, 0, 0, 0};
+// Cut tiles of logits: the shares added in order, then what head_softmax_tile makes of a whole tile.  A workgroup has 8 rows of a tile,
+// 8 columns per thread.
+__global__ void __launch_bounds__(256) head_logits_reduce_kernel(const float* __restrict__ part, HeadParams h, uint16_t* __restrict__ E,
+                                                                 int steps) {
+  const HeadShape shape = head_shape(h, h.col_tiles, steps);
+  const int n_tail = shape.tiles_m * h.col_tiles - shape.split.n_direct;
+  if ((int)blockIdx.x >= n_tail) return;
+  int tm, tn;
+  gemm_tile_of(shape.split.n_direct + (int)blockIdx.x, shape.tiles_m, h.col_tiles, tm, tn);
+  const int R = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), c = (int)(threadIdx.x & 31) * 8;
+  const int t = tm * kGemmBM + R, col = tn * kGemmBN + c;
+  if (t >= shape.rows) return;
+  const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
+  const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
+  float z[8] = {};
+  for (int k = 0; k < shape.split.splits; ++k, src += stride) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(src), b = *reinterpret_cast<const f32x4*>(src + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] += a[e];
+      z[4 + e] += b[e];
+    }
+  }
+  float m = -__builtin_huge_valf();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (col + e < h.vocab) m = fmaxf(m, z[e]);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float ref = head_reference(m);
+  const int y = h.target[t] - col;
+  if (y >= 0 && y < 8) {
+    float zy = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zy = y == e ? z[e] : zy;
+    h.target_logit[t] = zy;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    z[e] = col + e < h.vocab ? __builtin_amdgcn_exp2f((z[e] - ref) * 1.44269504088896340736f) : 0.f;
+    s += z[e];
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o, 64);
+  if (c == 0) h.stats[(int64_t)t * h.col_tiles + tn] = HeadStat{ref, s};
+  if (E && col < h.vocab) store8<true>(E, (int64_t)t * h.ld + col, z);
 }
 
-// The last vocab % 32 columns of W as rows of 32, zeros behind them.
-__global__ void __launch_bounds__(256) ce_tail_kernel(const uint16_t* __restrict__ W, int64_t ld, int d, int vocab,
-                                                      uint16_t* __restrict__ tail) {
-  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x, n = i >> 5, c = i & 31, v = vocab / 32 * 32 + c;
-  if (n < d) tail[i] = v < vocab ? W[(int64_t)n * ld + v] : (uint16_t)0;
+// dH rows of a piece whose tiles were cut: the shares in order, scaled, as gemm_reduce_kernel
+// The workgroups behind `tiles` make the job losses: all tokens' are known by then.
+__global__ void __launch_bounds__(256) head_grad_reduce_kernel(const float* __restrict__ part, HeadParams head, CeTokens c_tokens,
+                                                               uint16_t* __restrict__ out, const int32_t* __restrict__ out_index, int N,
+                                                               int tiles_n, int steps, int tiles, int num_jobs,
+                                                               float* __restrict__ job_loss) {
+  if ((int)blockIdx.x >= tiles) {
+    __shared__ double jobs_red[4];
+    const int j = ((int)blockIdx.x - tiles) * (int)gridDim.y + (int)blockIdx.y;
+    if (j >= num_jobs) return;
+    ce_job(c_tokens, j, 256, job_loss, [&](double x) {
+      x = wave_sum(x);
+      if ((threadIdx.x & 63) == 0) jobs_red[threadIdx.x >> 6] = x;
+      __syncthreads();
+      const double all = (jobs_red[0] + jobs_red[1]) + (jobs_red[2] + jobs_red[3]);
+      __syncthreads();
+      return all;
+    });
+    return;
+  }
+  const HeadShape h = head_shape(head, tiles_n, steps);
+  const int n_tail = h.tiles_m * tiles_n - h.split.n_direct;
+  if ((int)blockIdx.x >= n_tail) return;
+  int tm, tn;
+  gemm_tile_of(h.split.n_direct + (int)blockIdx.x, h.tiles_m, tiles_n, tm, tn);
+  const int R = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), c = (int)(threadIdx.x & 31) * 8;
+  const int t = tm * kGemmBM + R, col = tn * kGemmBN + c;
+  if (t >= h.rows || col >= N) return;
+  const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
+  const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
+  f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+  for (int k = 0; k < h.split.splits; ++k, src += stride) {
+    a += *reinterpret_cast<const f32x4*>(src);
+    b += *reinterpret_cast<const f32x4*>(src + 4);
+  }
+  const float f = head.factor[t];
+  if (f == 0.f) a = b = f32x4{0, 0, 0, 0};
+  a *= f;  b *= f;
+  *reinterpret_cast<u32x4*>(out + (int64_t)out_index[t] * N + col) =
+      u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
 }
 
 // A row's statistics become its logarithm of the sum and its loss; with GRAD its exponentials become those of the gradient: all
@@ -228,23 +341,39 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
 
 }  // namespace
 
-void launch_ce_prepare(const CeTokens& c, int num_jobs, const float* dloss, float* loss, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL(ce_prepare_kernel, dim3(1 + num_jobs), dim3(1024), 0, st, c, dloss, loss, lse);
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const int32_t* host_offsets, const CePrepare& p, hipStream_t st) {
+  const int row_groups = p.dH || p.rows ? (c.T + 15) / 16 : 0;
+  const dim3 grid(1 + num_jobs + row_groups + (p.W_tail ? (c.d + 31) / 32 : 0));
+  int32_t* const table = const_cast<int32_t*>(c.offsets);
+  CeOffsets args = {};
+  if (num_jobs <= kCeArgJobs) {
+    for (int j = 0; j <= num_jobs; ++j) args.at[j] = host_offsets[j];
+    hipLaunchKernelGGL(ce_prepare_kernel<true>, grid, dim3(1024), 0, st, c, num_jobs, table, args, p, row_groups);
+  } else {
+    launch_table_write(host_offsets, sizeof(int32_t) * ((size_t)num_jobs + 1), table, st);
+    hipLaunchKernelGGL(ce_prepare_kernel<false>, grid, dim3(1024), 0, st, c, num_jobs, table, args, p, row_groups);
+  }
 }
 void launch_ce_jobs(const CeTokens& c, int num_jobs, float* job_loss, hipStream_t st) {
   hipLaunchKernelGGL(ce_jobs_kernel, dim3(num_jobs), dim3(1024), 0, st, c, job_loss);
 }
 void launch_ce_gather(const HeadParams& h, const CeTokens& c, const uint16_t* H, uint16_t* rows, int d, hipStream_t st) {
-  hipLaunchKernelGGL(ce_gather_kernel, dim3((h.max_rows + 3) / 4), dim3(256), 0, st, h.live, h.first, h.max_rows, c.list,
-                     reinterpret_cast<const uint8_t*>(H), reinterpret_cast<uint8_t*>(rows), (int64_t)d * 2);
+  hipLaunchKernelGGL(ce_gather_kernel, dim3((h.max_rows + 3) / 4), dim3(256), 0, st, h.live, h.first, h.max_rows, c.list, H, rows, d);
 }
-void launch_ce_zero_rows(const CeTokens& c, uint16_t* dH, int d, hipStream_t st) {
-  if (c.T == 0) return;
-  hipLaunchKernelGGL(ce_zero_rows_kernel, dim3((c.T + 3) / 4), dim3(256), 0, st, c.targets, c.T, c.vocab,
-                     reinterpret_cast<uint8_t*>(dH), (int64_t)d * 2);
+// tiles that may be cut: less than a round
+static int head_cut_tiles(const HeadParams& h, int tiles_n) { return std::min((h.max_rows + kGemmBM - 1) / kGemmBM * tiles_n, 255); }
+void launch_head_logits_reduce(const HeadParams& h, uint16_t* E, int d, const float* part, hipStream_t st) {
+  if (d % kGemmBK) return;                             // (none is)
+  hipLaunchKernelGGL(head_logits_reduce_kernel, dim3(head_cut_tiles(h, h.col_tiles), std::min((h.max_rows + 7) / 8, kGemmBM / 8)), dim3(256), 0,
+                     st, part, h, E, d / kGemmBK);
 }
-void launch_ce_tail(const uint16_t* W, int64_t ld, int d, int vocab, uint16_t* tail, hipStream_t st) {
-  hipLaunchKernelGGL(ce_tail_kernel, dim3((d * 32 + 255) / 256), dim3(256), 0, st, W, ld, d, vocab, tail);
+void launch_head_grad_reduce(const HeadParams& h, const CeTokens& c, uint16_t* dH, const int32_t* out_index, int d, const float* part,
+                             int num_jobs, float* job_loss, hipStream_t st) {
+  const int tiles_n = (d + kGemmBN - 1) / kGemmBN, tiles = head_cut_tiles(h, tiles_n), y = std::min((h.max_rows + 7) / 8, kGemmBM / 8);
+  const int jobs = job_loss ? num_jobs : 0;
+  HeadParams head = h;
+  hipLaunchKernelGGL(head_grad_reduce_kernel, dim3(tiles + (jobs + y - 1) / y, y), dim3(256), 0, st, part, head, c, dH, out_index, d,
+                     tiles_n, (h.vocab + kGemmBK - 1) / kGemmBK, tiles, jobs, job_loss);
 }
 void launch_ce_finish(const HeadParams& h, const CeTokens& c, uint16_t* E, uint16_t* E_tail, float* factor, float* loss, float* lse,
                       hipStream_t st) {
