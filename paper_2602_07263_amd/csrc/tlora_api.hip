@@ -2082,7 +2082,6 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
 // ---- residual stream and norms between two blocks ------------------------------------------------------------
 namespace tlora {
 namespace {
-constexpr int kNormUnits = 512;               // wanted units of the column sums: two per CU
 struct NormPlan {
   int64_t T = 0;
   bool by_job = false;                        // units do not cross jobs
@@ -2102,15 +2101,22 @@ int norm_plan(const tlora_norm_t* p, NormPlan& N) {
     if (p->offsets[j + 1] < p->offsets[j] || p->offsets[j + 1] > TLORA_MAX_TOKENS) return TLORA_EINVAL;
   N.T = p->offsets[p->num_jobs];
   N.by_job = p->gates != nullptr;
-  N.unit_rows = (int)std::max<int64_t>(4, (N.T + kNormUnits - 1) / kNormUnits);
-  auto units = [&](int64_t rows) { return (rows + N.unit_rows - 1) / N.unit_rows; };
-  if (N.by_job)
-    for (int j = 0; j < p->num_jobs; ++j) N.units += units(p->offsets[j + 1] - p->offsets[j]);
-  else
-    N.units = units(N.T);
+  // Rows of a unit: as few as let all units run at a time (a few more of them than fit, as whole units of every job make them, take
+  // as long again: 516 units of 62 rows 405 us, 504 of 64 316).  Below 4 rows to a unit the partial sums are more than half as
+  // many bytes as the rows, which is taken for the shorter chain of rows while there are few.
+  const int64_t fit = norm_resident_units(p->dtype == TLORA_BF16, p->d_model);
+  auto count = [&]() {
+    auto units = [&](int64_t rows) { return (rows + N.unit_rows - 1) / N.unit_rows; };
+    if (!N.by_job) return units(N.T);
+    int64_t n = 0;
+    for (int j = 0; j < p->num_jobs; ++j) n += units(p->offsets[j + 1] - p->offsets[j]);
+    return n;
+  };
+  N.unit_rows = N.T <= 256 ? 1 : (int)std::max<int64_t>(4, (N.T + fit - 1) / fit);
+  for (int tries = 0; (N.units = count()) > fit && N.T > 256 && tries < 8; ++tries) N.unit_rows += (N.unit_rows + 31) / 32;
   size_t w = 0;
   auto place = [&](size_t bytes) { const size_t at = w;  w = align_up(w + bytes, 256);  return at; };
-  N.off_rows = place(sizeof(float) * 4 * (size_t)N.T);
+  N.off_rows = place(norm_in_registers(p->dtype == TLORA_BF16, p->d_model) ? 0 : sizeof(float) * 4 * (size_t)N.T);
   N.off_partial = place(sizeof(float) * 3 * (size_t)N.units * p->d_model);
   N.total = std::max<size_t>(w, 256);
   return TLORA_OK;
@@ -2222,12 +2228,19 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
   float* const partial = reinterpret_cast<float*>(ws + N.off_partial);
   {
     Timed t(TLORA_K_NORM, st);
-    norm_groups(p, N, 1, nullptr, false,
-                [&](const NormJobs& jobs, int rows, int) { launch_norm_bwd_rows(bf, a, jobs, g, rows, rows_at, st); });
-    if (sums) {
+    if (norm_in_registers(bf, p->d_model)) {
       norm_groups(p, N, N.unit_rows, nullptr, false, [&](const NormJobs& jobs, int, int units) {
-        launch_norm_bwd_cols(bf, a, jobs, g, units, N.unit_rows, rows_at, partial, st);
+        launch_norm_bwd_units(bf, a, jobs, g, units, N.unit_rows, sums ? partial : nullptr, st);
       });
+    } else {
+      norm_groups(p, N, 1, nullptr, false,
+                  [&](const NormJobs& jobs, int rows, int) { launch_norm_bwd_rows(bf, a, jobs, g, rows, rows_at, st); });
+      if (sums)
+        norm_groups(p, N, N.unit_rows, nullptr, false, [&](const NormJobs& jobs, int, int units) {
+          launch_norm_bwd_cols(bf, a, jobs, g, units, N.unit_rows, rows_at, partial, st);
+        });
+    }
+    if (sums) {
       // (with `idle` the units are numbered alike: a job without tokens has none)
       const bool gammas = dgamma_post || dgamma_pre;
       bool first = true;

@@ -58,6 +58,32 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
   return t;
 }
 
+// op over lanes l, l ^ 16, l ^ 32, l ^ 48, in registers (row swaps of the lane's value with itself).
+template <class Op>
+__device__ __forceinline__ float across_16_32(float x, const Op& op) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  x = op(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return op(__builtin_bit_cast(float, (uint32_t)h[0]), __builtin_bit_cast(float, (uint32_t)h[1]));
+}
+// Sum over the wave, in registers, in a fixed order; every lane gets it.  (By __shfl_xor, six exchanges through LDS, one after the
+// other, a norm's row took 0.4 us longer per sum.)
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_sum(float x) {      // of the lane's 16
+  x += dpp<0xB1>(x);       // lanes l ^ 1
+  x += dpp<0x4E>(x);       // l ^ 2
+  x += dpp<0x141>(x);      // the other four of eight
+  x += dpp<0x140>(x);      // the other eight of sixteen
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row_sum(x);
+  return across_16_32(x, [](float a, float b) { return a + b; });
+}
+
 // Tile L of the walk: groups of 4 row tiles, so that workgroups that run together share activation and weight panels.
 __device__ __forceinline__ void gemm_tile_of(int L, int tiles_m, int tiles_n, int& tm, int& tn) {
   constexpr int GM = 4;

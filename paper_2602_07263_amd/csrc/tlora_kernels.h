@@ -201,6 +201,11 @@ struct NormJobs {
   NormJob job[kNormJobs];
 };
 void launch_norm_fwd(bool bf16, const NormArgs& a, const NormJobs& jobs, int rows, void* H, void* Xn, hipStream_t st);
+bool norm_in_registers(bool bf16, int d);// the rows' width allows launch_norm_bwd_units, else the two launches behind it are taken
+int norm_resident_units(bool bf16, int d);
+// partial [units of all launches][3][d], or null: not wanted
+void launch_norm_bwd_units(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int units, int unit_rows,
+                           float* partial, hipStream_t st);
 // row_stats: 4 floats per row, or null: not wanted
 void launch_norm_bwd_rows(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int rows, float* row_stats,
                           hipStream_t st);

@@ -950,14 +950,6 @@ struct GemmParams {
   HeadParams head;
 };
 
-// op over lanes l, l ^ 16, l ^ 32, l ^ 48, in registers (row swaps of the lane's value with itself).
-template <class Op>
-__device__ __forceinline__ float across_16_32(float x, const Op& op) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-  x = op(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-  const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-  return op(__builtin_bit_cast(float, (uint32_t)h[0]), __builtin_bit_cast(float, (uint32_t)h[1]));
-}
 // What a tile of logits leaves of itself.  A lane holds tokens 16 i + l % 16 of its wave's 128 rows and features 4 (l / 16) .. + 3 of
 // each of the wave's four blocks of 16 columns.  The row's exponentials are taken relative to 0 where its largest logit in the tile
 // lies within kHeadPlain, so that the tiles of a row agree on the reference and the gradient's product can add them up as they are;

@@ -11,12 +11,7 @@
 namespace tlora {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
-}
-__device__ __forceinline__ double wave_sum(double x) {
+__device__ __forceinline__ double wave_sum_double(double x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
   return x;
@@ -28,7 +23,7 @@ __device__ __forceinline__ float wave_max(float x) {
 }
 // sum over the 1024 threads of a workgroup, every thread gets it; the order is fixed
 __device__ __forceinline__ double block_sum_1024(double x, double* red) {
-  x = wave_sum(x);
+  x = wave_sum_double(x);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
   double t = 0.0;
@@ -235,7 +230,7 @@ __global__ void __launch_bounds__(256) head_grad_reduce_kernel(const float* __re
     const int j = ((int)blockIdx.x - tiles) * (int)gridDim.y + (int)blockIdx.y;
     if (j >= num_jobs) return;
     ce_job(c_tokens, j, 256, job_loss, [&](double x) {
-      x = wave_sum(x);
+      x = wave_sum_double(x);
       if ((threadIdx.x & 63) == 0) jobs_red[threadIdx.x >> 6] = x;
       __syncthreads();
       const double all = (jobs_red[0] + jobs_red[1]) + (jobs_red[2] + jobs_red[3]);
@@ -454,6 +449,224 @@ __global__ void __launch_bounds__(256) norm_fwd_kernel(NormArgs a, NormJobs jobs
   }
 }
 
+// Rows of at most kNormRow features stay in registers: a thread has eight neighbouring features and the workgroup as many waves as
+// the row needs.  A lane behind the row's end repeats its last features with zeros for their values.
+constexpr int kNormRow = 8192;
+constexpr int norm_bwd_row(bool bf16) { return bf16 ? kNormRow : kNormRow / 2; }      // (fp32 operands take twice the registers)
+static int norm_threads(int d) { return (d / 8 + 63) / 64 * 64; }
+
+// Sums over the workgroup; each use between two barriers has a slot of its own.
+template <int N>
+__device__ __forceinline__ void norm_sums(float (&x)[N], float (*slot)[16]) {
+  const int waves = (int)blockDim.x >> 6, wave = (int)threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+  if (waves == 1) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if ((threadIdx.x & 63) == 0) slot[i][wave] = x[i];
+  __syncthreads();
+  const int w = (int)threadIdx.x & 15;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = row_sum(w < waves ? slot[i][w] : 0.f);
+}
+// Eight values as they lie in memory, fetched ahead of their use; p null: `other`.
+template <bool BF>
+struct Raw8 {
+  u32x4 v[BF ? 1 : 2];
+  __device__ __forceinline__ void fetch(const void* p, int64_t i) {
+    const char* const at = static_cast<const char*>(p) + i * (BF ? 2 : 4);
+#pragma unroll
+    for (int k = 0; k < (BF ? 1 : 2); ++k) v[k] = ldg16(at + 16 * k);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) {
+    // (kept as loaded until here: the compiler would convert right behind the load, and wait for it there)
+#pragma unroll
+    for (int k = 0; k < (BF ? 1 : 2); ++k) asm volatile("" : "+v"(v[k]));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (BF) {
+        x[2 * e] = __builtin_bit_cast(float, v[0][e] << 16);
+        x[2 * e + 1] = __builtin_bit_cast(float, v[0][e] & 0xffff0000u);
+      } else {
+        const uint32_t lo = v[0][e], hi = v[BF ? 0 : 1][e];     // (bit_cast of the element itself takes element 0)
+        x[e] = __builtin_bit_cast(float, lo);
+        x[4 + e] = __builtin_bit_cast(float, hi);
+      }
+    }
+  }
+};
+__device__ __forceinline__ void fill8(float (&x)[8], float v) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = v;
+}
+
+// A row per workgroup: bound by HBM (31744 x 4096 bf16 183 us, 5.7 TB/s; read again for each sum, 256).
+template <bool BF>
+__global__ void __launch_bounds__(1024) norm_fwd_row_kernel(NormArgs a, NormJobs jobs, void* __restrict__ H, void* __restrict__ Xn) {
+  __shared__ float red[2][1][16];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int64_t row = (int64_t)(jb.row0 + (int)blockIdx.x - jb.unit0) * a.d;
+  const bool on = (int)threadIdx.x * 8 < a.d;
+  const int c = on ? (int)threadIdx.x * 8 : a.d - 8;
+  float y[8], h[8], g[8], p[8], q[8];
+  load8<BF>(a.Y, row + c, y);
+  load8_or<BF>(a.X, row + c, 0.f, h);
+  load8_or<BF>(jb.gate, c, 1.f, g);
+  load8_or<BF>(a.gamma_post, c, 1.f, p);
+  load8_or<BF>(Xn ? a.gamma_pre : nullptr, c, 0.f, q);
+  float r1 = 1.f;
+  if (a.gamma_post) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[0] += y[e] * y[e];
+    if (!on) s[0] = 0.f;
+    norm_sums(s, red[0]);
+    r1 = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] += a.res_scale * (g[e] * (y[e] * r1 * p[e]));
+  if (H && on) store8<BF>(H, row + c, h);
+  if (!Xn) return;
+  float s[1] = {0.f};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[0] += h[e] * h[e];
+  if (!on) s[0] = 0.f;
+  norm_sums(s, red[1]);
+  const float r2 = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = h[e] * r2 * q[e];
+  if (on) store8<BF>(Xn, row + c, h);
+}
+
+// 1 / sqrt(x): the instruction's estimate and one Newton step
+__device__ __forceinline__ float rstd_of(float x) {
+  const float r = __builtin_amdgcn_rsqf(x);
+  return r * fmaf(-0.5f * x * r, r, 1.5f);
+}
+
+// Backward of a unit's rows, one after the other; with SUMS the unit's column sums stay in registers and leave as partial
+// [unit][3][d] (dgamma_post, dgamma_pre, dgate).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
+// for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
+// what the second sums give, D = dH + r2 (dXn gamma_pre) - k2 H, so the last sum is put together from three that need rstd_Y
+// alone; and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
+// barrier.  31744 x 4096 bf16 with all sums 316 us
+// (5.1 TB/s with the partial sums).
+// BOTH: dX and dY are wanted.  Every lane then stores without a condition -- those behind the row's end its last features once more,
+// the same values -- since behind a store that may not have been issued the compiler waits for all those that may.
+template <bool BF, bool SUMS, bool BOTH>
+__global__ void __launch_bounds__(norm_bwd_row(BF) / 8) norm_bwd_unit_kernel(NormArgs a, NormJobs jobs, NormGrads g, int unit_rows,
+                                                             float* __restrict__ partial) {
+  __shared__ float red[2][6][16];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int t0 = jb.row0 + ((int)blockIdx.x - jb.unit0) * unit_rows, t1 = min(t0 + unit_rows, jb.row1);
+  const bool on = (int)threadIdx.x * 8 < a.d;
+  const int c = on ? (int)threadIdx.x * 8 : a.d - 8;
+  const float inv_d = 1.0f / (float)a.d;
+  float agp[8], q[8];                        // res_scale * gate * gamma_post, and gamma_pre
+  {
+    float p[8];
+    load8_or<BF>(jb.gate, c, 1.f, agp);
+    load8_or<BF>(a.gamma_post, c, 1.f, p);
+    load8_or<BF>(a.gamma_pre, c, 0.f, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) agp[e] *= p[e] * a.res_scale;
+  }
+  // a job's gate and gamma_post are factors of whole columns: of D Y rstd_Y one sum serves both
+  float sum_y[8] = {}, sum_h[8] = {};
+  // (an operand that is not there is Y once more: around a branch in the loop the compiler would wait for all loads)
+  Raw8<BF> ry, rx, rh, rn;
+  const void *const X = a.X ? a.X : a.Y, *const dH = g.dH ? g.dH : a.Y, *const dXn = g.dXn ? g.dXn : a.Y;
+  auto fetch = [&](int t) {
+    const int64_t at = (int64_t)t * a.d + c;
+    rx.fetch(X, at);
+    rh.fetch(dH, at);
+    rn.fetch(dXn, at);
+  };
+  auto squares = [&](const float (&v)[8]) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[e] * v[e];
+    return on ? s : 0.f;
+  };
+  float y[8], r1 = 1.f;
+  ry.fetch(a.Y, (int64_t)t0 * a.d + c);
+  fetch(t0);
+  ry.get(y);
+  if (a.gamma_post) {
+    float s[1] = {squares(y)};
+    norm_sums(s, red[1]);
+    r1 = rstd_of(s[0] * inv_d + a.eps);
+  }
+  ry.fetch(a.Y, (int64_t)min(t0 + 1, t1 - 1) * a.d + c);
+  for (int t = t0; t < t1; ++t) {
+    const int64_t at = (int64_t)t * a.d + c;
+    float h[8], D[8], gq[8];
+    rx.get(h);
+    rh.get(D);
+    rn.get(gq);
+    fetch(min(t + 1, t1 - 1));
+    if (!a.X) fill8(h, 0.f);
+    if (!g.dH) fill8(D, 0.f);
+    if (!g.dXn) fill8(gq, 0.f);
+    float s[6] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[e] += agp[e] * (y[e] * r1);
+      const float w = agp[e] * y[e], u = gq[e] * q[e];
+      s[0] += h[e] * h[e];
+      s[1] += u * h[e];
+      s[2] += D[e] * w;
+      s[3] += u * w;
+      s[4] += h[e] * w;
+    }
+    float next[8];
+    ry.get(next);
+    ry.fetch(a.Y, (int64_t)min(t + 2, t1 - 1) * a.d + c);
+    s[5] = squares(next);
+#pragma unroll
+    for (int i = 0; i < 5; ++i) s[i] = on ? s[i] : 0.f;
+    norm_sums(s, red[(t - t0) & 1]);
+    float r2 = 0.f, k2 = 0.f;
+    if (g.dXn) {
+      r2 = rstd_of(s[0] * inv_d + a.eps);
+      k2 = s[1] * r2 * r2 * r2 * inv_d;
+    }
+    const float k1 = a.gamma_post ? (s[2] + r2 * s[3] - k2 * s[4]) * r1 * r1 * r1 * inv_d : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      D[e] += r2 * (gq[e] * q[e]) - h[e] * k2;
+      if (SUMS) {
+        sum_y[e] += D[e] * (y[e] * r1);
+        sum_h[e] += gq[e] * (h[e] * r2);
+      }
+    }
+    if (BOTH || g.dX) store8<BF>(g.dX, at, D);
+    if (BOTH || g.dY) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D[e] = r1 * (agp[e] * D[e]) - y[e] * k1;
+      store8<BF>(g.dY, at, D);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = next[e];
+    if (a.gamma_post) r1 = rstd_of(s[5] * inv_d + a.eps);
+  }
+  if (SUMS && on) {
+    float* const o = partial + (int64_t)(jobs.unit_base + (int)blockIdx.x) * 3 * a.d + c;
+    float p[8], gate[8], v[8];
+    load8_or<BF>(jb.gate, c, 1.f, gate);
+    load8_or<BF>(a.gamma_post, c, 1.f, p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gate[e] * a.res_scale * sum_y[e];
+    store8<false>(o, 0, v);
+    store8<false>(o, a.d, sum_h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[e] * a.res_scale * sum_y[e];
+    store8<false>(o, 2 * (int64_t)a.d, v);
+  }
+}
+
+// ---- wider rows: read again for every sum -----------------------------------------------------------------------------------
 // rstd of Y and of H, and the factor of H in D = dH + r2 (dXn gamma_pre) - H k2
 struct NormRow {
   float r1, r2, k2, pad;
@@ -593,8 +806,18 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* __restri
   if (!out) return;
   const int per = (u1 - u0 + 15) / 16, a = u0 + slice * per, b = min(a + per, u1);
   float s = 0.f;
-  if (c < d)
-    for (int u = a; u < b; ++u) s += partial[((int64_t)u * 3 + k) * d + c];
+  if (c < d) {
+    const float* p = partial + ((int64_t)a * 3 + k) * d + c;
+    int u = a;
+    for (; u + 8 <= b; u += 8, p += 24 * (int64_t)d) {       // eight loads in flight
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p[3 * (int64_t)d * i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    for (; u < b; ++u, p += 3 * (int64_t)d) s += *p;
+  }
   red[slice][x] = s;
   __syncthreads();
   if (slice == 0 && c < d) {
@@ -608,8 +831,33 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* __restri
 
 void launch_norm_fwd(bool bf16, const NormArgs& a, const NormJobs& jobs, int rows, void* H, void* Xn, hipStream_t st) {
   if (rows == 0) return;
+  if (a.d <= kNormRow) {
+    const dim3 block(norm_threads(a.d));
+    if (bf16) hipLaunchKernelGGL(norm_fwd_row_kernel<true>, dim3(rows), block, 0, st, a, jobs, H, Xn);
+    else      hipLaunchKernelGGL(norm_fwd_row_kernel<false>, dim3(rows), block, 0, st, a, jobs, H, Xn);
+    return;
+  }
   if (bf16) hipLaunchKernelGGL(norm_fwd_kernel<true>, dim3(rows), dim3(256), 0, st, a, jobs, H, Xn);
   else      hipLaunchKernelGGL(norm_fwd_kernel<false>, dim3(rows), dim3(256), 0, st, a, jobs, H, Xn);
+}
+bool norm_in_registers(bool bf16, int d) { return d <= norm_bwd_row(bf16); }
+// Workgroups of the backward that the chip holds at a time: 16 waves to a CU, as its registers allow, or 8 for fp32.
+int norm_resident_units(bool bf16, int d) {
+  return norm_in_registers(bf16, d) ? 256 * (bf16 ? 16 : 8) / (norm_threads(d) / 64) : 512;
+}
+void launch_norm_bwd_units(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int units, int unit_rows,
+                           float* partial, hipStream_t st) {
+  if (units == 0) return;
+  const dim3 block(norm_threads(a.d));
+  const bool both = g.dX && g.dY;
+#define TLORA_NORM_BWD(BF, SUMS)                                                                                              \
+  do {                                                                                                                      \
+    if (both) hipLaunchKernelGGL((norm_bwd_unit_kernel<BF, SUMS, true>), dim3(units), block, 0, st, a, jobs, g, unit_rows, partial);  \
+    else      hipLaunchKernelGGL((norm_bwd_unit_kernel<BF, SUMS, false>), dim3(units), block, 0, st, a, jobs, g, unit_rows, partial); \
+  } while (0)
+  if (bf16) { if (partial) TLORA_NORM_BWD(true, true);  else TLORA_NORM_BWD(true, false); }
+  else      { if (partial) TLORA_NORM_BWD(false, true); else TLORA_NORM_BWD(false, false); }
+#undef TLORA_NORM_BWD
 }
 void launch_norm_bwd_rows(bool bf16, const NormArgs& a, const NormJobs& jobs, const NormGrads& g, int rows, float* row_stats,
                           hipStream_t st) {
