@@ -125,7 +125,7 @@ struct HeadParams {
 };
 constexpr int kHeadMaxSplits = 16;
 constexpr int kHeadShare = 8;            // K-steps
-constexpr size_t kHeadPartBytes = (size_t)256 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most one round of tiles
+constexpr size_t kHeadPartBytes = (size_t)512 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most two rounds of tiles
 // Largest logit of a row in a tile up to which exp(z) needs no reference, and from which on sums of it hold their digits.
 __host__ __device__ inline float head_reference(float m) {
   constexpr float kTop = 60.f, kBottom = -40.f;

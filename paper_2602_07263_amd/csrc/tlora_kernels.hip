@@ -1517,9 +1517,9 @@ void launch_seg_gemm(bool w_is_kn, const TileDev* tiles, const uint16_t* act, co
 #undef TLORA_GEMM_LAUNCH
 }
 
-// As many workgroups as the most that any number of rows asks for: whole rounds, and one of shares.
+// As many workgroups as the most that any number of rows asks for: whole rounds, and two of shares.
 static dim3 head_grid(const HeadParams& head, int tiles_n) {
-  return dim3((head.max_rows + kGemmBM - 1) / kGemmBM * tiles_n / 256 * 256 + 256);
+  return dim3((head.max_rows + kGemmBM - 1) / kGemmBM * tiles_n / 256 * 256 + 512);
 }
 void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, float* part, hipStream_t st) {
   GemmParams P = {};
