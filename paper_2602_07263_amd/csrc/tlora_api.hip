@@ -1143,14 +1143,22 @@ struct Copies {
   bool a_all = false;                                   // A_j side by side
   bool wt = false;                                      // W^T
 };
+// X in 8 bits: dA_j is made from the codes as they are
+struct PackedX {
+  const uint8_t* codes = nullptr;
+  const uint16_t* scales = nullptr;
+  int groups = 0;
+};
 // The backward's launch sequence (out_index / in_index as in fwd_impl: dX rows are scattered; X and dY are fetched
 // through the list; shared_sums as there, also for the partial tiles of dA / dB; later as there, the product then follows the
 // gradients).
 // copies: of the nano-batches before this one, brought up to date (null: no nano-batch).
 // batch_tokens: of the whole batch, if the call is one of its nano-batches.  It decides whether dX has use for a copy of W^T.
+// packed: what dA_j is made from instead of X, which is not read then (bf16, S_j kept).
 int bwd_impl(const tlora_problem_t* p, const void* dY, void* dX, void* const* dA, void* const* dB, int flags,
              void* workspace, size_t ws_bytes, void* hip_stream, const int32_t* out_index, const int32_t* in_index,
-             uint8_t* shared_sums = nullptr, GemmCall* later = nullptr, Copies* copies = nullptr, int64_t batch_tokens = 0) {
+             uint8_t* shared_sums = nullptr, GemmCall* later = nullptr, Copies* copies = nullptr, int64_t batch_tokens = 0,
+             const PackedX& packed = PackedX()) {
   const PlanEntry* entry = nullptr;
   std::vector<JobDev> hjobs;
   int rc = common_checks(p, &entry, hjobs, workspace, ws_bytes, false, shared_sums != nullptr);
@@ -1319,7 +1327,8 @@ int bwd_impl(const tlora_problem_t* p, const void* dY, void* dX, void* const* dA
   }
   if (want_grads) {
     const GradSide b = {reinterpret_cast<const GradUnit*>(tb + pl.tb_gBu), Shi, Slo, dYb, pl.d_out, (int)pl.gradB_units.size()};
-    const GradSide a = {reinterpret_cast<const GradUnit*>(tb + pl.tb_gAu), dShi, dSlo, Xb, pl.d_in, (int)pl.gradA_units.size()};
+    const GradSide a = {reinterpret_cast<const GradUnit*>(tb + pl.tb_gAu), dShi, dSlo, Xb, pl.d_in, (int)pl.gradA_units.size(),
+                        packed.codes, packed.scales, packed.groups};
     const GradSide none;
     auto gradients = [&](const GradSide& dB_side, const GradSide& dA_side) {
       Timed t(TLORA_K_RANK_GRAD, st);
@@ -2479,11 +2488,18 @@ int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY,
     for (int j = 0; j < p->num_jobs; ++j)
       if (p->ranks[j] > 0 && (!dA[j] || !dB[j])) return TLORA_ENULL;
   if (flags & ~(TLORA_BWD_REUSE_S | TLORA_BWD_REUSE_WT | TLORA_BWD_ACCUMULATE)) return TLORA_EINVAL;
-  if (dA) {                       // (X enters the adapters' gradients alone)
+  // X enters the adapters' gradients alone: dA_j, which the codes serve as they are (rows of whole 16-byte pieces), and S_j, where it
+  // is to be made again, which takes the values
+  PackedX x;
+  if (dA && p->dtype == TLORA_BF16 && (flags & TLORA_BWD_REUSE_S) && p->d_in % 16 == 0) {
+    x.codes = static_cast<const uint8_t*>(packed);
+    x.scales = reinterpret_cast<const uint16_t*>(x.codes + ckpt_scales_at(T, p->d_in));
+    x.groups = (p->d_in + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
+  } else if (dA) {
     rc = tlora_ckpt_unpack(p->dtype, packed, T, p->d_in, X, hip_stream);
     if (rc != TLORA_OK) return rc;
   }
-  return tlora_bwd(&q, dY, dX, dA, dB, flags, workspace, inner, hip_stream);
+  return bwd_impl(&q, dY, dX, dA, dB, flags, workspace, inner, hip_stream, nullptr, nullptr, nullptr, nullptr, nullptr, 0, x);
 }
 
 // ---- general token -> adapter assignment (Sec. 3.3: tokens of an adapter are gathered, results scattered back) ----

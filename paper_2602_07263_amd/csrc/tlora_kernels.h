@@ -100,6 +100,10 @@ struct GradSide {
   const GradUnit* units = nullptr;
   const uint16_t *Uhi = nullptr, *Ulo = nullptr, *V = nullptr;      // V: [T, D], rows through row_index if that is given
   int D = 0, count = 0;
+  // instead of V, of a without row_index: 8-bit codes [T, D], D a multiple of 16, and their scales, bf16 [T, groups]
+  const uint8_t* codes = nullptr;
+  const uint16_t* scales = nullptr;
+  int groups = 0;
 };
 void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, float* partial, bool accumulate,
                       const int32_t* row_index, hipStream_t st);

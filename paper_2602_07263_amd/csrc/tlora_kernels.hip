@@ -1876,21 +1876,57 @@ __device__ __forceinline__ bf16x8 frag_tr_u(const uint8_t* plane, int pitch, int
 // the eight would idle, and a stage's U planes are a quarter, so that seven stages fit: a launch of few units waits for its loads, and
 // six steps in flight instead of three bring them sooner (one job of 512 tokens, 64 units: 12.6 us with four stages, now 9.4; 576
 // units of 4096 tokens 50.2 / 44.4; same bits).
-template <bool ONE>
+// Q8: V are 8-bit codes with a scale per row and 128 columns (activations kept in 8 bits).  Half the bytes of V come from memory; a
+// fragment is one transposing read of bytes and becomes bf16 on the way to the matrix instruction, as the unpacked tensor would
+// have it.  The scales of a unit's tokens for its two groups of columns are put into LDS first.  7680 tokens of four jobs, 4096 ->
+// 4096, S kept: unpacking 19 us and dA / dB 27 us, now 36; a call of 31744 tokens, 4096 -> 12288, without dX 484 us, now 429.  What is
+// left above half of the bf16 time is the conversion: about 3 vector operations per value, in each of the two waves that read it.
+template <bool ONE, bool Q8 = false>
 struct GradShape {
   static constexpr int MB = ONE ? 1 : kGradMaxBlocks;       // blocks of 32 ranks a U tile has room for;
   static constexpr int RP = kGradRanks * MB;                // a unit multiplies only its u.mb live ones
   static constexpr int UPLANE = kGradStep * 2 * RP;         // 2 KB * MB
-  static constexpr int VTILE = kGradStep * kGradCols * 2;   // 16 KB
+  static constexpr int VTILE = kGradStep * kGradCols * (Q8 ? 1 : 2);   // 16 KB (8 KB)
   static constexpr int STAGE = VTILE + 2 * UPLANE;
   static constexpr int STAGES = ONE ? 7 : 4;
 };
 constexpr int kGradLds = std::max(GradShape<true>::STAGE * GradShape<true>::STAGES, GradShape<false>::STAGE * GradShape<false>::STAGES);
 
-template <bool INDEXED, bool ONE>
+// Eight codes of the rows kb .. kb + 7 of a lane's column as bf16: 32 x 256 code tile, 256 bytes per row, 16-byte chunk c of row k at
+// slot c ^ 2 (k & 7) (the 8 rows x 32 bytes that two groups of 16 lanes read together lie in 16 distinct bank groups).
+// With 128 added a code is a byte that one instruction makes a float; (code + 128) s - 128 s in one rounding is exactly code s.
+struct CodeScales {
+  float s[8], offset[8];
+  __device__ __forceinline__ void get(const uint16_t* scales) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(scales);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[2 * i] = __builtin_bit_cast(float, v[i] << 16);
+      s[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) offset[i] = -128.f * s[i];
+  }
+};
+__device__ __forceinline__ bf16x8 frag_codes(const uint8_t* tile, const CodeScales& sc, int nb, int kb, int lane) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  const int s = lane & 15, k = kb + (s >> 1), c = (nb >> 4) + ((lane >> 4) & 1);
+  const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, tile + k * 256 + ((c ^ ((k & 7) << 1)) << 4) + (s & 1) * 8));
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t word = (uint32_t)w[e >> 2] ^ 0x80808080u;
+    v[e] = fmaf((float)((word >> (8 * (e & 3))) & 0xffu), sc.s[e], sc.offset[e]);
+  }
+  return as_bf16x8(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+}
+
+template <bool INDEXED, bool ONE, bool Q8>
 __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& jb, const GradSide& side, bool dA, float* partial,
-                                               int accumulate, const int32_t* row_index, uint8_t* lds, int32_t* srow) {
-  using G = GradShape<ONE>;
+                                               int accumulate, const int32_t* row_index, uint8_t* lds, int32_t* srow,
+                                               uint16_t (*scale)[kGradMaxTokens]) {
+  static_assert(!(INDEXED && Q8), "no such call");
+  using G = GradShape<ONE, Q8>;
   constexpr int MB = G::MB, RP = G::RP, UPLANE = G::UPLANE, VTILE = G::VTILE, STAGE = G::STAGE, STAGES = G::STAGES;
   constexpr int UPITCH = 2 * RP;                            // 256 (64) bytes per token row of a U tile
   // 16-byte chunk c of token row k sits at slot c ^ ((k & 3) << 2) so that the four rows one transposing read
@@ -1928,9 +1964,14 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
 #pragma unroll
   for (int i = 0; i < V_LD; ++i) {
     const int p = (wave * V_LD + i) * 64 + lane;
-    vk[i] = p >> 5;
-    const int c = (p & 31) ^ ((vk[i] & 3) << 2);
-    vcol[i] = min(col0 + c * 8, D - 8);               // columns beyond D are clamped; their results are not stored
+    if (Q8) {
+      vk[i] = p >> 4;
+      vcol[i] = min(col0 + ((p & 15) ^ ((vk[i] & 7) << 1)) * 16, D - 16);
+    } else {
+      vk[i] = p >> 5;
+      const int c = (p & 31) ^ ((vk[i] & 3) << 2);
+      vcol[i] = min(col0 + c * 8, D - 8);             // columns beyond D are clamped; their results are not stored
+    }
   }
   // U tiles: hi plane then lo plane, 2 * MB KB each = 2 * MB wave-loads; wave w issues loads q = w * U_LD + i of the
   // 4 * MB.  Lanes whose rank chunk lies beyond rpad fetch nothing: the stale slots only feed rank rows >= rpad
@@ -1954,6 +1995,13 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
     for (int i = tid; i < min(u.t1 - u.t0, kGradMaxTokens); i += WAVES * 64) srow[i] = row_index[u.t0 + i];
     __syncthreads();
   }
+  if (Q8) {                                           // (rows beyond the unit's last are that one again, like the codes)
+    for (int i = tid; i < 2 * nsteps * kGradStep; i += WAVES * 64) {
+      const int t = min(u.t0 + (i >> 1), u.t1 - 1), g = min(col0 / 128 + (i & 1), side.groups - 1);
+      scale[i & 1][i >> 1] = side.scales[(int64_t)t * side.groups + g];
+    }
+    __syncthreads();
+  }
   int f_step = 0;                                     // next step to fetch
   auto issue = [&](int stage) {
     uint8_t* const S = lds + stage * STAGE;
@@ -1964,21 +2012,26 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
     for (int i = 0; i < V_LD; ++i) {
       int t = min(u.t0 + st * kGradStep + vk[i], u.t1 - 1);
       if (INDEXED) t = srow[min(t - u.t0, kGradMaxTokens - 1)];
-      dma16(V + (int64_t)t * D + vcol[i], sbase + i * 1024);
+      if (Q8) dma16(side.codes + (int64_t)t * D + vcol[i], sbase + i * 1024);
+      else    dma16(V + (int64_t)t * D + vcol[i], sbase + i * 1024);
     }
 #pragma unroll
     for (int i = 0; i < U_LD; ++i)
       if (ulive[i]) dma16(usrc[i] + (int64_t)st * kGradStep * jb.rpad, hbase + __builtin_amdgcn_readfirstlane(udst[i]));
     ++f_step;
   };
+  int c_step = 0;                                     // next step to multiply (Q8: where its scales are)
   auto compute = [&](int stage) {
     const uint8_t* const S = lds + stage * STAGE;
     const uint8_t* const H = S + VTILE;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       bf16x8 vf[NW];
+      CodeScales sc;
+      if (Q8) sc.get(scale[wcol >> 7] + c_step * kGradStep + kk * 16 + (lane >> 5) * 8);
 #pragma unroll
-      for (int n = 0; n < NW; ++n) vf[n] = frag_kn_tile(S, wcol + n * 32, kk, lane);
+      for (int n = 0; n < NW; ++n)
+        vf[n] = Q8 ? frag_codes(S, sc, wcol + n * 32, kk * 16 + (lane >> 5) * 8, lane) : frag_kn_tile(S, wcol + n * 32, kk, lane);
 #pragma unroll
       for (int i = 0; i < MW; ++i) {
         const int m = rh + 2 * i;
@@ -1993,6 +2046,7 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
         }
       }
     }
+    ++c_step;
   };
   auto landed = [&]() {
     // loads complete in order: all but those of the youngest steps have landed
@@ -2104,7 +2158,7 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
 // others leave partial tiles.  With partial tiles for every job and a launch for each side, dA and dB took, reductions included (mlp
 // projections of 31744 tokens 797 us / now 723; 32 skewed jobs 1695 / 1501; four jobs of 7680 tokens, 4096 -> 4096, 54 / 43; three of
 // 9082, 4096 -> 5120, 94 / 58; 4198 tokens of eleven jobs, 10848 -> 1448, 77 / 52).
-template <bool INDEXED>
+template <bool INDEXED, bool Q8>                        // Q8: the V of dA
 __global__ void __launch_bounds__(512) rank_grad_kernel(const JobDev* __restrict__ jobs, GradSide side, GradSide a_side,
                                                         float* __restrict__ partial, int accumulate,
                                                         const int32_t* __restrict__ row_index) {
@@ -2112,12 +2166,19 @@ __global__ void __launch_bounds__(512) rank_grad_kernel(const JobDev* __restrict
   // token-indexed calls: where in the batch each token row of the unit lies (row_index of the unit's chunk, staged
   // once so that the load loop never waits for an index from memory; a unit has at most kGradMaxTokens tokens)
   __shared__ int32_t srow[INDEXED ? kGradMaxTokens : 1];
+  __shared__ __attribute__((aligned(16))) uint16_t scale[2][Q8 ? kGradMaxTokens : 1];
   const bool dA = (int)blockIdx.x >= side.count;
   if (dA) side = a_side;
   const GradUnit u = side.units[dA ? blockIdx.x - (gridDim.x - a_side.count) : blockIdx.x];
   const JobDev jb = jobs[u.job];
-  if (u.mb == 1) rank_grad_unit<INDEXED, true>(u, jb, side, dA, partial, accumulate, row_index, lds, srow);
-  else           rank_grad_unit<INDEXED, false>(u, jb, side, dA, partial, accumulate, row_index, lds, srow);
+  auto* const sc = reinterpret_cast<uint16_t(*)[kGradMaxTokens]>(scale);
+  if (Q8 && dA) {
+    if (u.mb == 1) rank_grad_unit<false, true, Q8>(u, jb, side, true, partial, accumulate, nullptr, lds, srow, sc);
+    else           rank_grad_unit<false, false, Q8>(u, jb, side, true, partial, accumulate, nullptr, lds, srow, sc);
+    return;
+  }
+  if (u.mb == 1) rank_grad_unit<INDEXED, true, false>(u, jb, side, dA, partial, accumulate, row_index, lds, srow, sc);
+  else           rank_grad_unit<INDEXED, false, false>(u, jb, side, dA, partial, accumulate, row_index, lds, srow, sc);
 }
 
 void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, float* partial, bool accumulate,
@@ -2125,8 +2186,9 @@ void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, 
   if (a.count + b.count == 0) return;
   const dim3 grid(a.count + b.count);
   const int add = accumulate ? 1 : 0;
-  if (row_index) hipLaunchKernelGGL(rank_grad_kernel<true>, grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
-  else           hipLaunchKernelGGL(rank_grad_kernel<false>, grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
+  if (a.codes)        hipLaunchKernelGGL((rank_grad_kernel<false, true>), grid, dim3(512), 0, st, jobs, b, a, partial, add, nullptr);
+  else if (row_index) hipLaunchKernelGGL((rank_grad_kernel<true, false>), grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
+  else                hipLaunchKernelGGL((rank_grad_kernel<false, false>), grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
 }
 
 // Sum the partial tiles of one output tile in unit order (bit-reproducible), scale, and store (dB_j row-major [r, D];
