@@ -354,8 +354,8 @@ def tlora_bwd(prob: tlora_problem_t, dY_ptr: int, dX_ptr: int, dA_ptrs: Optional
 
 
 def _ptr(t):
-    """Device address of a tensor; None for no tensor or an empty one."""
-    return ctypes.c_void_p(t.data_ptr()) if t is not None and t.numel() else None
+    """Device address of a tensor; None for no tensor or an empty one (torch's address of that is 0)."""
+    return (t.data_ptr() or None) if t is not None else None
 
 
 def _grad_ptr_arrays(J, dA_ptrs, dB_ptrs):
@@ -834,7 +834,7 @@ class ResidualNorm:
         self.ws = None               # (made by the first bwd: a forward has no use for it)
 
     def _stream(self):
-        return ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream))
+        return self.torch.cuda.current_stream().cuda_stream
 
     def fwd(self, H, Xn) -> None:
         _check(lib().tlora_norm_fwd(ctypes.byref(self.prob), _ptr(H), _ptr(Xn), self._stream()), "tlora_norm_fwd")
@@ -844,8 +844,7 @@ class ResidualNorm:
             self.ws = self.torch.empty(self.ws_bytes, dtype=self.torch.uint8, device=self._keep[1].device)
         g = None if dgates is None else (ctypes.c_void_p * self.J)(*[_ptr(t) for t in dgates])
         _check(lib().tlora_norm_bwd(ctypes.byref(self.prob), _ptr(dH), _ptr(dXn), _ptr(dX), _ptr(dY), _ptr(dgamma_post),
-                                    _ptr(dgamma_pre), g, int(flags), ctypes.c_void_p(self.ws.data_ptr()),
-                                    ctypes.c_size_t(self.ws_bytes), self._stream()), "tlora_norm_bwd")
+                                    _ptr(dgamma_pre), g, int(flags), self.ws.data_ptr(), self.ws_bytes, self._stream()), "tlora_norm_bwd")
 
 
 class LossHead:
@@ -868,8 +867,7 @@ class LossHead:
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=W.device)
 
     def _tail(self):
-        return (ctypes.c_void_p(self.ws.data_ptr()), ctypes.c_size_t(self.ws_bytes),
-                ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream)))
+        return self.ws.data_ptr(), self.ws_bytes, self.torch.cuda.current_stream().cuda_stream
 
     def fwd(self, loss, lse, job_loss) -> None:
         _check(lib().tlora_ce_fwd(ctypes.byref(self.prob), _ptr(loss), _ptr(lse), _ptr(job_loss), *self._tail()), "tlora_ce_fwd")
@@ -891,7 +889,7 @@ class Checkpoint:
         self.packed = torch.empty(n, dtype=torch.uint8, device=device)
 
     def _stream(self):
-        return ctypes.c_void_p(int(self.torch.cuda.current_stream().cuda_stream))
+        return self.torch.cuda.current_stream().cuda_stream
 
     def pack(self, X) -> None:
         _check(lib().tlora_ckpt_pack(self.code, _ptr(X), self.T, self.d, _ptr(self.packed), self._stream()), "tlora_ckpt_pack")
