@@ -2393,8 +2393,9 @@ int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, floa
 }  // namespace
 
 size_t tlora_ce_workspace_bytes(const tlora_ce_t* p, int32_t with_grad) {
-  CePlan C;
-  return ce_plan(p, with_grad != 0, C) == TLORA_OK ? C.total : 0;
+  CePlan C, G;                                             // (one for the gradient serves the losses alone too)
+  if (ce_plan(p, false, C) != TLORA_OK) return 0;
+  return with_grad && ce_plan(p, true, G) == TLORA_OK ? std::max(C.total, G.total) : C.total;
 }
 int tlora_ce_fwd(const tlora_ce_t* p, float* loss, float* lse, float* job_loss, void* workspace, size_t ws_bytes, void* hip_stream) {
   return ce_run(p, false, nullptr, loss, lse, job_loss, nullptr, workspace, ws_bytes, hip_stream);

@@ -539,10 +539,11 @@ __global__ void __launch_bounds__(1024) norm_fwd_row_kernel(NormArgs a, NormJobs
   if (on) store8<BF>(Xn, row + c, h);
 }
 
-// 1 / sqrt(x): the instruction's estimate and one Newton step
+// 1 / sqrt(x): the instruction's estimate and one Newton step (which has no say about 0 and infinity)
 __device__ __forceinline__ float rstd_of(float x) {
   const float r = __builtin_amdgcn_rsqf(x);
-  return r * fmaf(-0.5f * x * r, r, 1.5f);
+  const float better = r * fmaf(-0.5f * x * r, r, 1.5f);
+  return x > 0.f && x < __builtin_huge_valf() ? better : r;
 }
 
 // Backward of a unit's rows, one after the other; with SUMS the unit's column sums stay in registers and leave as partial

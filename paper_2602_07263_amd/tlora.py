@@ -358,6 +358,13 @@ def _ptr(t):
     return (t.data_ptr() or None) if t is not None else None
 
 
+def _dense(tensors, dtypes, what: str) -> None:
+    """The tensors of a holder have to be what the struct says of them: dense, of these dtypes (None: no tensor)."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_contiguous() or (dtypes[name] is not None and t.dtype != dtypes[name])):
+            raise TloraError(f"{what}: {name} must be contiguous" + (f" {dtypes[name]}" if dtypes[name] is not None else ""))
+
+
 def _grad_ptr_arrays(J, dA_ptrs, dB_ptrs):
     if dA_ptrs is None:
         return None, None
@@ -824,6 +831,9 @@ class ResidualNorm:
         J = len(self.offsets) - 1
         self.J, self.d = J, int(Y.shape[1])
         self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
+        vectors = {f"gates[{j}]": g for j, g in enumerate(gates or [])}
+        tensors = dict(X=X, Y=Y, gamma_pre=gamma_pre, gamma_post=gamma_post, **vectors)
+        _dense(tensors, dict.fromkeys(tensors, torch.bfloat16 if dtype == "bf16" else torch.float32), "ResidualNorm")
         self._gates = None if gates is None else (ctypes.c_void_p * J)(*[_ptr(g) for g in gates])
         self._keep = [X, Y, gamma_pre, gamma_post, gates]
         self.prob = tlora_norm_t(TLORA_BF16 if dtype == "bf16" else TLORA_F32, J, self.d, self._off, float(eps), float(res_scale),
@@ -858,6 +868,8 @@ class LossHead:
         self.offsets = [int(o) for o in offsets]
         J = len(self.offsets) - 1
         self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
+        _dense(dict(H=H, W=W, targets=targets, weights=weights),
+               dict(H=torch.bfloat16, W=torch.bfloat16, targets=torch.int32, weights=torch.float32), "LossHead")
         self._keep = [H, W, targets, weights]
         self.prob = tlora_ce_t(TLORA_BF16, J, int(W.shape[0]), int(vocab), int(W.shape[1]), self._off, _ptr(H), _ptr(W),
                                _ptr(targets), _ptr(weights))
@@ -891,10 +903,18 @@ class Checkpoint:
     def _stream(self):
         return self.torch.cuda.current_stream().cuda_stream
 
+    def _check(self, X) -> None:
+        t = self.torch
+        _dense(dict(X=X), dict(X=t.bfloat16 if self.code == TLORA_BF16 else t.float32), "Checkpoint")
+        if X.numel() != self.T * self.d:
+            raise TloraError("Checkpoint: X has another size")
+
     def pack(self, X) -> None:
+        self._check(X)
         _check(lib().tlora_ckpt_pack(self.code, _ptr(X), self.T, self.d, _ptr(self.packed), self._stream()), "tlora_ckpt_pack")
 
     def unpack(self, X) -> None:
+        self._check(X)
         _check(lib().tlora_ckpt_unpack(self.code, _ptr(self.packed), self.T, self.d, _ptr(X), self._stream()),
                "tlora_ckpt_unpack")
 

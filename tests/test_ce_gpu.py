@@ -205,6 +205,23 @@ def test_pieces_of_a_long_batch():
     _check(out, r, H, W, y, V)
 
 
+def test_more_jobs_than_an_argument_takes_and_one_workspace_for_both_calls():
+    import torch
+    rng = np.random.default_rng(2)
+    tokens = rng.integers(0, 4, 300)
+    off, T = np.concatenate([[0], np.cumsum(tokens)]), int(tokens.sum())
+    H, W, y = _inputs(40, T, 512, 200, 200)
+    r = _oracle(H, W, y, 200, off)
+    head = _head(H, W, y, 200, off)
+    out, ev = _outs(head), _outs(head)
+    head.fwd_bwd(*out)
+    head.fwd(*ev[:3])
+    torch.cuda.synchronize()
+    _check(out, r, H, W, y, 200)
+    for a, b in zip(ev[:3], out[:3]):
+        assert torch.equal(a, b)
+
+
 def test_repeated_calls_give_the_same_bits_on_a_larger_workspace_and_another_stream():
     import torch
     off = [0, 200, 517]

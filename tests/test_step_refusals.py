@@ -148,3 +148,25 @@ def test_backward_from_eight_bits_refuses():
     assert rc(mk(dtype=3)) == -3 and rc(mk(d=60)) == -1 and rc(mk(W=0)) == -2 and rc(mk(B=0)) == -2
     assert L.tlora_ckpt_workspace_bytes(ctypes.byref(mk(d=60)[0])) == 0
     assert L.tlora_bwd_ckpt(None, P(WS), P(0x5000), None, None, None, 0, P(WS), BIG, None) == -2
+
+
+def test_a_workspace_for_the_gradient_serves_the_losses_alone():
+    L = tlora.lib()
+    for T, d, V, ld in ((10000, 8192, 1000, 1000), (100, 64, 9, 16), (50000, 1024, 50000, 50000)):
+        q = _ce((T,), d, V, ld)
+        assert L.tlora_ce_workspace_bytes(ctypes.byref(q), 1) >= L.tlora_ce_workspace_bytes(ctypes.byref(q), 0) > 0
+
+
+def test_holders_refuse_tensors_of_another_layout_or_type():
+    import torch
+    bf = torch.bfloat16
+    H, W, y = torch.zeros(4, 16, dtype=bf), torch.zeros(16, 24, dtype=bf), torch.zeros(4, dtype=torch.int32)
+    for args in ((H, torch.zeros(24, 16, dtype=bf).t(), y), (H.float(), W, y), (H, W, y.long())):
+        with pytest.raises(tlora.TloraError, match="LossHead"):
+            tlora.LossHead([0, 4], args[0], args[1], 20, args[2])
+    with pytest.raises(tlora.TloraError, match="weights"):
+        tlora.LossHead([0, 4], H, W, 20, y, weights=torch.zeros(4, dtype=torch.float64))
+    with pytest.raises(tlora.TloraError, match="gates"):
+        tlora.ResidualNorm("bf16", [0, 4], H, H, None, 1e-5, gates=[torch.zeros(16)])
+    with pytest.raises(tlora.TloraError, match="Checkpoint"):
+        tlora.Checkpoint("bf16", 4, 16, "cpu").pack(H.t())
