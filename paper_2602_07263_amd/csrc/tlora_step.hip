@@ -43,8 +43,14 @@ __device__ __forceinline__ double block_sum_1024(double x, double* red) {
 __device__ __forceinline__ bool ce_live(int y, int vocab) { return (unsigned)y < (unsigned)vocab; }
 
 __device__ __forceinline__ void copy_row(const uint16_t* src, uint16_t* dst, int d, int lane) {     // src null: zeros
-  for (int i = lane * 8; i < d; i += 512)
-    *reinterpret_cast<u32x4*>(dst + i) = src ? ldg16(src + i) : u32x4{0, 0, 0, 0};
+  for (int i = lane * 8; i < d; i += 4096) {           // eight loads in flight: a row of 4096 takes one latency, not eight
+    u32x4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = src ? ldg16(src + min(i + k * 512, d - 8)) : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i + k * 512 < d) *reinterpret_cast<u32x4*>(dst + i + k * 512) = v[k];
+  }
 }
 
 template <bool ARGS>
@@ -185,6 +191,7 @@ __global__ void __launch_bounds__(256) head_logits_reduce_kernel(const float* __
   const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
   const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
   float z[8] = {};
+#pragma unroll 4
   for (int k = 0; k < shape.split.splits; ++k, src += stride) {
     const f32x4 a = *reinterpret_cast<const f32x4*>(src), b = *reinterpret_cast<const f32x4*>(src + 4);
 #pragma unroll
@@ -250,6 +257,7 @@ __global__ void __launch_bounds__(256) head_grad_reduce_kernel(const float* __re
   const int64_t stride = (int64_t)n_tail * kGemmBM * kGemmBN;
   const float* src = part + ((int64_t)blockIdx.x * kGemmBM + R) * kGemmBN + c;
   f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+#pragma unroll 8
   for (int k = 0; k < h.split.splits; ++k, src += stride) {
     a += *reinterpret_cast<const f32x4*>(src);
     b += *reinterpret_cast<const f32x4*>(src + 4);
