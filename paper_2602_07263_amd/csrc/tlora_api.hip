@@ -808,7 +808,7 @@ void launch_gemm_pair(const GemmCall& a, const GemmCall& b, hipStream_t st) {
 // S_j = X_j.A_j (or dS_j = dY_j.B_j^T): streaming kernel when the contraction length allows, else generic
 void run_shrink(const Plan& pl, const uint8_t* tb, const JobDev* jobs, const TileDev* tiles, const uint16_t* act, int K,
                 const uint16_t* packed, bool packed_is_atp, uint16_t* hi, uint16_t* lo, uint16_t* Sx,
-                const int32_t* row_index, float* part, hipStream_t st) {
+                const int32_t* row_index, float* part, hipStream_t st, const PackedX& codes = PackedX()) {
   const int splits = packed_is_atp ? pl.shrink_splits_x : pl.shrink_splits_dy;
   if (splits > 1) {
     launch_shrink_split(jobs, tiles, reinterpret_cast<const ShrinkUnit*>(tb + pl.tb_stream), (int)pl.stream_units.size(),
@@ -816,13 +816,22 @@ void run_shrink(const Plan& pl, const uint8_t* tb, const JobDev* jobs, const Til
     return;
   }
   launch_zero_fill(Sx, 2 * (size_t)pl.sx_elems, st);
-  if (K % 32 == 0)
+  if (codes.codes)
+    launch_shrink_codes(jobs, tiles, reinterpret_cast<const ShrinkUnit*>(tb + pl.tb_stream), (int)pl.stream_units.size(), pl.shrink_rows,
+                        codes, K, packed, packed_is_atp, hi, lo, Sx, st);
+  else if (K % 32 == 0)
     launch_shrink_stream(jobs, tiles, reinterpret_cast<const ShrinkUnit*>(tb + pl.tb_stream),
                          (int)pl.stream_units.size(), pl.shrink_rows, g_opt.shrink_stages, act, K, packed, packed_is_atp,
                          hi, lo, Sx, row_index, st);
   else
     launch_shrink(jobs, tiles, reinterpret_cast<const ShrinkUnit*>(tb + pl.tb_shrink), (int)pl.shrink_units.size(), 64,
                   act, K, packed, packed_is_atp, hi, lo, Sx, row_index, st);
+}
+
+// Whether S_j = X_j.A_j can be made from codes of X: the streaming kernel's long steps, scales that fit beside its stages.
+bool shrink_takes_codes(const Plan& pl) {
+  const int64_t groups = (pl.d_in + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
+  return pl.shrink_splits_x == 1 && !pl.small_x && pl.d_in % 64 == 0 && pl.shrink_rows >= 64 && groups * pl.shrink_rows <= kShrinkScales;
 }
 
 int check_arch() {
@@ -1143,18 +1152,12 @@ struct Copies {
   bool a_all = false;                                   // A_j side by side
   bool wt = false;                                      // W^T
 };
-// X in 8 bits: dA_j is made from the codes as they are
-struct PackedX {
-  const uint8_t* codes = nullptr;
-  const uint16_t* scales = nullptr;
-  int groups = 0;
-};
 // The backward's launch sequence (out_index / in_index as in fwd_impl: dX rows are scattered; X and dY are fetched
 // through the list; shared_sums as there, also for the partial tiles of dA / dB; later as there, the product then follows the
 // gradients).
 // copies: of the nano-batches before this one, brought up to date (null: no nano-batch).
 // batch_tokens: of the whole batch, if the call is one of its nano-batches.  It decides whether dX has use for a copy of W^T.
-// packed: what dA_j is made from instead of X, which is not read then (bf16, S_j kept).
+// packed: what dA_j, and S_j if it is to be made again (shrink_takes_codes), are made from instead of X, which is not read then (bf16).
 int bwd_impl(const tlora_problem_t* p, const void* dY, void* dX, void* const* dA, void* const* dB, int flags,
              void* workspace, size_t ws_bytes, void* hip_stream, const int32_t* out_index, const int32_t* in_index,
              uint8_t* shared_sums = nullptr, GemmCall* later = nullptr, Copies* copies = nullptr, int64_t batch_tokens = 0,
@@ -1292,7 +1295,7 @@ int bwd_impl(const tlora_problem_t* p, const void* dY, void* dX, void* const* dA
         launch_small(true, jobs, tiles, xf.out ? xf.out : Xb, nullptr, atp, bp, pl.r_total, nullptr, nullptr, in_index, pl.T, pl.d_in, pl.d_out,
                      pl.small_x, partial, Shi, Slo, st);
       } else {
-        run_shrink(pl, tb, jobs, tiles, Xb, pl.d_in, atp, true, Shi, Slo, Sx, in_index, partial, st);
+        run_shrink(pl, tb, jobs, tiles, Xb, pl.d_in, atp, true, Shi, Slo, Sx, in_index, partial, st, packed);
       }
     }
     if (small) {
@@ -1328,7 +1331,7 @@ int bwd_impl(const tlora_problem_t* p, const void* dY, void* dX, void* const* dA
   if (want_grads) {
     const GradSide b = {reinterpret_cast<const GradUnit*>(tb + pl.tb_gBu), Shi, Slo, dYb, pl.d_out, (int)pl.gradB_units.size()};
     const GradSide a = {reinterpret_cast<const GradUnit*>(tb + pl.tb_gAu), dShi, dSlo, Xb, pl.d_in, (int)pl.gradA_units.size(),
-                        packed.codes, packed.scales, packed.groups};
+                        packed};
     const GradSide none;
     auto gradients = [&](const GradSide& dB_side, const GradSide& dA_side) {
       Timed t(TLORA_K_RANK_GRAD, st);
@@ -2489,10 +2492,10 @@ int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY,
     for (int j = 0; j < p->num_jobs; ++j)
       if (p->ranks[j] > 0 && (!dA[j] || !dB[j])) return TLORA_ENULL;
   if (flags & ~(TLORA_BWD_REUSE_S | TLORA_BWD_REUSE_WT | TLORA_BWD_ACCUMULATE)) return TLORA_EINVAL;
-  // X enters the adapters' gradients alone: dA_j, which the codes serve as they are (rows of whole 16-byte pieces), and S_j, where it
-  // is to be made again, which takes the values
+  // X enters the adapters' gradients alone: dA_j, and S_j where it is to be made again.  The codes serve both as they are where rows are
+  // whole 16-byte pieces and the shrink is a streaming one; a small batch's forms of it take the values.
   PackedX x;
-  if (dA && p->dtype == TLORA_BF16 && (flags & TLORA_BWD_REUSE_S) && p->d_in % 16 == 0) {
+  if (dA && p->dtype == TLORA_BF16 && p->d_in % 16 == 0 && ((flags & TLORA_BWD_REUSE_S) || shrink_takes_codes(entry->pl))) {
     x.codes = static_cast<const uint8_t*>(packed);
     x.scales = reinterpret_cast<const uint16_t*>(x.codes + ckpt_scales_at(T, p->d_in));
     x.groups = (p->d_in + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;

@@ -63,6 +63,17 @@ void launch_shrink_stream(const JobDev* jobs, const TileDev* tiles, const Shrink
                           int shrink_rows, int stages, const uint16_t* act, int K, const uint16_t* packed,
                           bool packed_is_atp, uint16_t* S_hi, uint16_t* S_lo, uint16_t* Sx, const int32_t* row_index,
                           hipStream_t st);
+// An activation [T, D] kept in 8 bits: codes [T, D] and scales, bf16 [T, groups], of 128 values each.
+struct PackedX {
+  const uint8_t* codes = nullptr;        // null: there is none
+  const uint16_t* scales = nullptr;
+  int groups = 0;
+};
+// Same result from codes (K % 64 == 0, units of 64 or 128 rows, at most kShrinkScales scales in a unit's rows).
+constexpr int kShrinkScales = 20480;
+void launch_shrink_codes(const JobDev* jobs, const TileDev* tiles, const ShrinkUnit* units, int num_units, int shrink_rows,
+                         const PackedX& codes, int K, const uint16_t* packed, bool packed_is_atp, uint16_t* S_hi, uint16_t* S_lo,
+                         uint16_t* Sx, hipStream_t st);
 // Same result with the contraction cut into `splits` (K % 64 == 0, units of 32 rows; splits <= K / 64): `part` holds
 // `splits` copies of part_stride floats (>= the packed S elements).  Writes all of Sx, zeros included: no fill needed.
 void launch_shrink_split(const JobDev* jobs, const TileDev* tiles, const ShrinkUnit* units, int num_units, int splits, int T,
@@ -100,10 +111,7 @@ struct GradSide {
   const GradUnit* units = nullptr;
   const uint16_t *Uhi = nullptr, *Ulo = nullptr, *V = nullptr;      // V: [T, D], rows through row_index if that is given
   int D = 0, count = 0;
-  // instead of V, of a without row_index: 8-bit codes [T, D], D a multiple of 16, and their scales, bf16 [T, groups]
-  const uint8_t* codes = nullptr;
-  const uint16_t* scales = nullptr;
-  int groups = 0;
+  PackedX packed;                                                   // instead of V, of a without row_index; D a multiple of 16
 };
 void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, float* partial, bool accumulate,
                       const int32_t* row_index, hipStream_t st);

@@ -94,6 +94,18 @@ __device__ __forceinline__ bf16x8 frag_row32(const uint8_t* tile, int rb, int kk
   return as_bf16x8(*reinterpret_cast<const u32x4*>(tile + row32_off(r, kk * 2 + (lane >> 5))));
 }
 
+// Eight 8-bit codes with their scales, and those times -128, as bf16.
+// With 128 added a code is a byte that one instruction makes a float; (code + 128) s - 128 s in one rounding is exactly code s.
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t w0, uint32_t w1, const float (&s)[8], const float (&offset)[8]) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t word = (e < 4 ? w0 : w1) ^ 0x80808080u;
+    v[e] = fmaf((float)((word >> (8 * (e & 3))) & 0xffu), s[e], offset[e]);
+  }
+  return as_bf16x8(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+}
+
 // MFMA operand fragment of a kn tile: columns nb .. nb+31, k-step kk, through the transposing LDS read
 // (ds_read_b64_tr_b16: inside each group of 16 lanes, lane i receives element (i % 4) of the 8-byte
 // rows addressed by lanes 4e + i/4, e = 0..3 -- i.e. 4 consecutive k for column i of a 4 x 16 block).
@@ -560,6 +572,10 @@ constexpr int waitcnt_vm_lgkm0(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 
 // (128 x 32); NS stages are filled NS - 1 steps ahead by raw asynchronous global->LDS loads, so several KB
 // per wave stay in flight without holding registers -- the kernel is bound by how fast X (or dY) streams in.
 // ---------------------------------------------------------------------------------------------------
+// Q8: the activations are 8-bit codes with a scale per row and 128 values (activations kept in 8 bits): half the bytes of X, which
+// become bf16 on the way to the matrix instruction, as the unpacked tensor would have them.  The scales of a unit's rows are put
+// into LDS first (kShrinkScales of them at most).  31744 x 4096, ranks 4 to 128: 59 us, as long as from bf16 (a step's chain of barrier,
+// reads, conversion and products sets the pace), without the 65 us of unpacking before it.
 // PCOLS: rank columns staged per step.  A unit whose job has at most 32 (64) padded rank columns stages such an
 // adapter tile and spends the LDS it saves on more stages: the kernel is bound by the bytes of X in flight.
 // WAVES: 4, or 8 for the 128-row units.  A CU runs one workgroup (the stages fill its LDS), so with four waves every
@@ -570,14 +586,16 @@ constexpr int waitcnt_vm_lgkm0(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 
 // loads each wave issues.  For a 32-column unit waves 4-7 only help to load.
 // SPLIT: the unit contracts only the K-steps [step0, step0 + nsteps) and leaves its fp32 sums in `part` (the packed
 // ragged layout of the planes, one copy per split), which shrink_emit_kernel adds up in split order.
-template <int ROWS, int NS, int KS, int PCOLS, int WAVES, bool SPLIT>
+template <int ROWS, int NS, int KS, int PCOLS, int WAVES, bool SPLIT, bool Q8 = false>
 __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUnit u, const JobDev jb,
                                                    const TileDev* __restrict__ tiles,
                                                    const uint16_t* __restrict__ act, int K,
                                                    const uint16_t* __restrict__ packed, int packed_is_atp,
                                                    uint16_t* __restrict__ Shi, uint16_t* __restrict__ Slo,
                                                    uint16_t* __restrict__ Sx, const int32_t* __restrict__ row_index,
-                                                   int step0, int nsteps, float* __restrict__ part) {
+                                                   int step0, int nsteps, float* __restrict__ part,
+                                                   const PackedX& codes = PackedX(), uint16_t* scale = nullptr) {
+  static_assert(!Q8 || (KS == 64 && !SPLIT), "a step of codes lies in one group");
   constexpr int WM = ROWS / 32;                    // waves along token rows
   constexpr int CW = PCOLS == 128 ? WAVES : WM * (PCOLS / 32);   // waves that multiply
   constexpr int WN = CW / WM;                      // waves along rank columns
@@ -586,7 +604,7 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
   static_assert(WN >= 1 && PW % 32 == 0 && NPB >= 1, "wave layout");
   constexpr int RB = KS * 2;                       // bytes per tile row: 64 (K-steps of 32) or 128 (of 64)
   constexpr int CPR = RB / 16;                     // 16-byte chunks per tile row
-  constexpr int A_BYTES = ROWS * RB, P_BYTES = PCOLS * RB, STAGE = A_BYTES + P_BYTES;
+  constexpr int A_BYTES = Q8 ? ROWS * KS : ROWS * RB, P_BYTES = PCOLS * RB, STAGE = A_BYTES + P_BYTES;
   constexpr int A_TOT = A_BYTES / 1024, P_TOT = P_BYTES / 1024;            // 1 KB wave-loads per tile
   constexpr int A_LD = A_TOT / WAVES, P_LD = (P_TOT + WAVES - 1) / WAVES;   // loads per wave per step
   static_assert(kGemmBM == 256, "the row -> GEMM tile lookup below shifts by 8");
@@ -609,7 +627,8 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
 
   // lane -> (row, 16-byte chunk) of the 64-byte-row tiles; rows beyond the unit / beyond rpad are clamped
   // (they only feed outputs that are not stored, or that are stored as zeros)
-  const uint16_t* asrc[A_LD];
+  const uint8_t* asrc[A_LD];
+  constexpr int A_STEP = Q8 ? KS : 2 * KS;         // bytes of a row and step
   const uint16_t* psrc[P_LD];
   int pslot[P_LD];         // which 1 KB piece of the adapter tile this wave's load i fills (when the tile has fewer
                            // pieces than there are waves, the upper waves repeat the lower waves' loads: same bytes
@@ -618,10 +637,11 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
                            // columns); lane 0 always fetches so every wave issues the same number of loads
 #pragma unroll
   for (int i = 0; i < A_LD; ++i) {
-    const int q = (wave * A_LD + i) * 64 + lane, r = q / CPR;
-    const int c = KS == 32 ? (q & 3) ^ ((r >> 2) & 3) : (q & 7) ^ ((r >> 1) & 7);
+    const int q = (wave * A_LD + i) * 64 + lane, r = q / (Q8 ? 4 : CPR);
+    const int c = KS == 32 || Q8 ? (q & 3) ^ ((r >> 2) & 3) : (q & 7) ^ ((r >> 1) & 7);
     const int t = u.t0 + min(r, u.nrows - 1);      // token row of the job-sorted order; row_index: where it lies
-    asrc[i] = act + (int64_t)(row_index ? row_index[t] : t) * K + c * 8 + (SPLIT ? (int64_t)step0 * KS : 0);
+    asrc[i] = Q8 ? codes.codes + (int64_t)t * K + c * 16
+                 : reinterpret_cast<const uint8_t*>(act + (int64_t)(row_index ? row_index[t] : t) * K + c * 8 + (SPLIT ? (int64_t)step0 * KS : 0));
   }
 #pragma unroll
   for (int i = 0; i < P_LD; ++i) {
@@ -639,12 +659,19 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
     const bool needed = !SPLIT || f_step < nsteps || lane == 0;      // (a split has few steps)
 #pragma unroll
     for (int i = 0; i < A_LD; ++i)
-      if (needed) dma16(asrc[i] + st * KS, base + (wave * A_LD + i) * 1024);
+      if (needed) dma16(asrc[i] + (int64_t)st * A_STEP, base + (wave * A_LD + i) * 1024);
 #pragma unroll
     for (int i = 0; i < P_LD; ++i)
       if (plive[i] && needed) dma16(psrc[i] + st * KS, base + A_BYTES + __builtin_amdgcn_readfirstlane(pslot[i]) * 1024);
     ++f_step;
   };
+  if (Q8) {                                        // scale[group][row]
+    for (int i = tid; i < ROWS * codes.groups; i += WAVES * 64) {
+      const int r = i / codes.groups, g = i - r * codes.groups;
+      scale[g * ROWS + r] = codes.scales[(int64_t)(u.t0 + min(r, u.nrows - 1)) * codes.groups + g];
+    }
+    __syncthreads();
+  }
   for (int i = 0; i < NS - 1; ++i) issue();
   for (int kt = 0; kt < nsteps; ++kt) {
     // loads complete in order: all but those of the NS - 2 youngest steps have landed
@@ -656,9 +683,23 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
       // all fragments of the step first, then the MFMAs: a read -> wait -> MFMA chain per k-slice would pay the LDS
       // latency KS / 16 times per step
       bf16x8 xf[KS / 16], pf[KS / 16][NPB];
+      float sc[8], off[8];
+      if (Q8) {                                    // the lane's row has one scale for the step
+        const float s = bf16_float(scale[(kt >> 1) * ROWS + wm * 32 + (lane & 31)]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sc[e] = s;
+          off[e] = -128.f * s;
+        }
+      }
 #pragma unroll
       for (int kk = 0; kk < KS / 16; ++kk) {
-        xf[kk] = KS == 32 ? frag_row32(S, wm * 32, kk, lane) : frag_row_tile(S, wm * 32, kk, lane);
+        if (Q8) {                                  // 64-byte rows of 16-byte pieces, of which half a wave has one half
+          const u32x2 w = *reinterpret_cast<const u32x2*>(S + row32_off(wm * 32 + (lane & 31), kk) + (lane >> 5) * 8);
+          xf[kk] = codes_bf16(w[0], w[1], sc, off);
+        } else {
+          xf[kk] = KS == 32 ? frag_row32(S, wm * 32, kk, lane) : frag_row_tile(S, wm * 32, kk, lane);
+        }
 #pragma unroll
         for (int i = 0; i < NPB; ++i)
           pf[kk][i] = KS == 32 ? frag_row32(S + A_BYTES, wn * PW + i * 32, kk, lane)
@@ -740,6 +781,40 @@ __device__ __forceinline__ void shrink_stream_body(uint8_t* lds, const ShrinkUni
     }
     if (which < 2) __syncthreads();
   }
+}
+
+constexpr int kShrinkScaleBytes = kShrinkScales * 2;
+template <int ROWS, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) shrink_codes_kernel(const JobDev* __restrict__ jobs, const TileDev* __restrict__ tiles,
+                                                                  const ShrinkUnit* __restrict__ units, PackedX codes, int K,
+                                                                  const uint16_t* __restrict__ packed, int packed_is_atp,
+                                                                  uint16_t* __restrict__ Shi, uint16_t* __restrict__ Slo,
+                                                                  uint16_t* __restrict__ Sx) {
+  constexpr int NS = 5, NS_LOW = 8;                // stages of (ROWS codes, 128 rank rows), of (ROWS codes, 32 rank rows)
+  constexpr int BYTES = std::max(NS * (ROWS * 64 + 128 * 128), NS_LOW * (ROWS * 64 + 32 * 128));
+  static_assert(BYTES + kShrinkScaleBytes <= 160 * 1024, "LDS of a CU");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[BYTES];
+  __shared__ uint16_t scale[kShrinkScales];
+  const ShrinkUnit u = units[blockIdx.x];
+  const JobDev jb = jobs[u.job];
+  if (ROWS == 128 && jb.rpad <= 32)
+    shrink_stream_body<128, NS_LOW, 64, 32, 8, false, true>(lds, u, jb, tiles, nullptr, K, packed, packed_is_atp, Shi, Slo, Sx, nullptr,
+                                                            0, K / 64, nullptr, codes, scale);
+  else
+    shrink_stream_body<ROWS, NS, 64, 128, WAVES, false, true>(lds, u, jb, tiles, nullptr, K, packed, packed_is_atp, Shi, Slo, Sx, nullptr,
+                                                              0, K / 64, nullptr, codes, scale);
+}
+void launch_shrink_codes(const JobDev* jobs, const TileDev* tiles, const ShrinkUnit* units, int num_units, int shrink_rows,
+                         const PackedX& codes, int K, const uint16_t* packed, bool packed_is_atp, uint16_t* S_hi, uint16_t* S_lo,
+                         uint16_t* Sx, hipStream_t st) {
+  if (num_units == 0) return;
+  const int atp = packed_is_atp ? 1 : 0;
+  if (shrink_rows == 128)
+    hipLaunchKernelGGL((shrink_codes_kernel<128, 8>), dim3(num_units), dim3(512), 0, st, jobs, tiles, units, codes, K, packed, atp, S_hi,
+                       S_lo, Sx);
+  else
+    hipLaunchKernelGGL((shrink_codes_kernel<64, 4>), dim3(num_units), dim3(256), 0, st, jobs, tiles, units, codes, K, packed, atp, S_hi,
+                       S_lo, Sx);
 }
 
 template <int ROWS, int NS, int KS, int WAVES>
@@ -1894,7 +1969,6 @@ constexpr int kGradLds = std::max(GradShape<true>::STAGE * GradShape<true>::STAG
 
 // Eight codes of the rows kb .. kb + 7 of a lane's column as bf16: 32 x 256 code tile, 256 bytes per row, 16-byte chunk c of row k at
 // slot c ^ 2 (k & 7) (the 8 rows x 32 bytes that two groups of 16 lanes read together lie in 16 distinct bank groups).
-// With 128 added a code is a byte that one instruction makes a float; (code + 128) s - 128 s in one rounding is exactly code s.
 struct CodeScales {
   float s[8], offset[8];
   __device__ __forceinline__ void get(const uint16_t* scales) {
@@ -1912,13 +1986,7 @@ __device__ __forceinline__ bf16x8 frag_codes(const uint8_t* tile, const CodeScal
   typedef int i32x2 __attribute__((ext_vector_type(2)));
   const int s = lane & 15, k = kb + (s >> 1), c = (nb >> 4) + ((lane >> 4) & 1);
   const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, tile + k * 256 + ((c ^ ((k & 7) << 1)) << 4) + (s & 1) * 8));
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t word = (uint32_t)w[e >> 2] ^ 0x80808080u;
-    v[e] = fmaf((float)((word >> (8 * (e & 3))) & 0xffu), sc.s[e], sc.offset[e]);
-  }
-  return as_bf16x8(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+  return codes_bf16((uint32_t)w[0], (uint32_t)w[1], sc.s, sc.offset);
 }
 
 template <bool INDEXED, bool ONE, bool Q8>
@@ -1997,8 +2065,8 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
   }
   if (Q8) {                                           // (rows beyond the unit's last are that one again, like the codes)
     for (int i = tid; i < 2 * nsteps * kGradStep; i += WAVES * 64) {
-      const int t = min(u.t0 + (i >> 1), u.t1 - 1), g = min(col0 / 128 + (i & 1), side.groups - 1);
-      scale[i & 1][i >> 1] = side.scales[(int64_t)t * side.groups + g];
+      const int t = min(u.t0 + (i >> 1), u.t1 - 1), g = min(col0 / 128 + (i & 1), side.packed.groups - 1);
+      scale[i & 1][i >> 1] = side.packed.scales[(int64_t)t * side.packed.groups + g];
     }
     __syncthreads();
   }
@@ -2012,7 +2080,7 @@ __device__ __forceinline__ void rank_grad_unit(const GradUnit& u, const JobDev& 
     for (int i = 0; i < V_LD; ++i) {
       int t = min(u.t0 + st * kGradStep + vk[i], u.t1 - 1);
       if (INDEXED) t = srow[min(t - u.t0, kGradMaxTokens - 1)];
-      if (Q8) dma16(side.codes + (int64_t)t * D + vcol[i], sbase + i * 1024);
+      if (Q8) dma16(side.packed.codes + (int64_t)t * D + vcol[i], sbase + i * 1024);
       else    dma16(V + (int64_t)t * D + vcol[i], sbase + i * 1024);
     }
 #pragma unroll
@@ -2186,7 +2254,7 @@ void launch_rank_grad(const JobDev* jobs, const GradSide& b, const GradSide& a, 
   if (a.count + b.count == 0) return;
   const dim3 grid(a.count + b.count);
   const int add = accumulate ? 1 : 0;
-  if (a.codes)        hipLaunchKernelGGL((rank_grad_kernel<false, true>), grid, dim3(512), 0, st, jobs, b, a, partial, add, nullptr);
+  if (a.packed.codes) hipLaunchKernelGGL((rank_grad_kernel<false, true>), grid, dim3(512), 0, st, jobs, b, a, partial, add, nullptr);
   else if (row_index) hipLaunchKernelGGL((rank_grad_kernel<true, false>), grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
   else                hipLaunchKernelGGL((rank_grad_kernel<false, false>), grid, dim3(512), 0, st, jobs, b, a, partial, add, row_index);
 }

@@ -84,7 +84,10 @@ LAYERS = [("bf16", 256, 384, [3, 16, 40, 0, 130], [70, 300, 129, 40, 260], [2.0,
           ("bf16", 512, 512, [8, 5], [70, 33], [2.0, 3.0]), ("f32", 136, 72, [4, 7], [50, 81], [2.0, 1.0]),
           ("bf16", 136, 1024, [1, 128, 32], [0, 700, 65], [1.0, 1.0, 2.0]),
           # a last tile of 16 columns, units of more tokens than one takes, ranks of several blocks
-          ("bf16", 272, 64, [40, 4], [9000, 31], [1.0, 2.0]), ("bf16", 144, 128, [200], [130], [1.0])]
+          ("bf16", 272, 64, [40, 4], [9000, 31], [1.0, 2.0]), ("bf16", 144, 128, [200], [130], [1.0]),
+          # batches whose S_j is made again from the codes: units of 64 and of 128 rows, low and high ranks, a half group at the end
+          ("bf16", 320, 64, [40, 130, 8], [7000, 5000, 301], [1.0, 2.0, 0.5]),
+          ("bf16", 448, 64, [16, 64, 160], [20000, 4001, 2300], [1.0, 2.0, 0.5])]
 
 
 @pytest.mark.parametrize("case", LAYERS, ids=[f"{c[0]}_{c[1]}_{c[2]}_{sum(c[4])}" for c in LAYERS])
