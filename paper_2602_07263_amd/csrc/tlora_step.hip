@@ -891,73 +891,102 @@ void launch_norm_reduce(const float* partial, const NormJobs& jobs, int first_ve
 }
 
 // ---------------------------------------------------------------------------------------------------
-// Activations in 8 bits: 16 lanes of 8 values have a group of 128.  Bound by memory.
+// Activations in 8 bits: 16 lanes of 8 values have a group of 128; a thread has four groups' values in flight.  Bound by memory (31744 x
+// 12288 bf16: packing 230 us, 5.1 TB/s, unpacking 193 us, 6.1 TB/s; one group at a time and the maximum by exchanges through LDS, 259
+// and 197).
 // ---------------------------------------------------------------------------------------------------
 namespace {
 
-// Where a thread's values lie: row, group of the row, first column; the workgroup has 16 consecutive groups.
+// Where a thread's values lie: row, group of the row, first column.  A workgroup has kCkptGroups consecutive groups, 16 at a time.
+constexpr int kCkptSteps = 4, kCkptGroups = 16 * kCkptSteps;
 struct CkptPlace {
   int64_t row, group;      // group: over all rows
   int col;
   bool on;
 };
-__device__ __forceinline__ CkptPlace ckpt_place(int64_t T, int d, int groups) {
-  const int64_t g0 = (int64_t)blockIdx.x * 16;
+__device__ __forceinline__ CkptPlace ckpt_place(int64_t T, int d, int groups, int step) {
+  const int64_t g0 = (int64_t)blockIdx.x * kCkptGroups;
   const int64_t r0 = g0 / groups;
-  const int g = (int)(g0 - r0 * groups) + (int)(threadIdx.x >> 4), more = g / groups;
+  const int i = step * 16 + (int)(threadIdx.x >> 4), g = (int)(g0 - r0 * groups) + i, more = g / groups;
   CkptPlace p;
   p.row = r0 + more;
-  p.group = g0 + (threadIdx.x >> 4);
+  p.group = g0 + i;
   p.col = (g - more * groups) * 128 + (int)(threadIdx.x & 15) * 8;
   p.on = p.row < T && p.col < d;
   return p;
+}
+// the largest of a lane's 16, in registers
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
 }
 
 template <bool BF>
 __global__ void __launch_bounds__(256) ckpt_pack_kernel(const void* __restrict__ X, int64_t T, int d, int groups,
                                                         uint8_t* __restrict__ codes, uint16_t* __restrict__ scales) {
-  const CkptPlace p = ckpt_place(T, d, groups);
-  float v[8] = {};
-  if (p.on) load8<BF>(X, p.row * d + p.col, v);
-  // the largest magnitude as an integer: infinities and NaN are the largest of all
-  uint32_t top = 0;
+  Raw8<BF> raw[kCkptSteps];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  const float amax = __builtin_bit_cast(float, top);
-  const bool finite = top < 0x7f000000u;               // below 2^127: 127 s, rounded, stays finite
-  auto up = [](float x) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) + 0xffffu) & 0xffff0000u); };
-  float s = up(amax / 127.0f);
-  if (127.0f * s < amax) s = up(s * (1.0f + 0x1p-12f));  // (127 s is exact: the quotient had been rounded down onto the grid)
-  s = fmaxf(s, 0x1p-100f);
-  const float inv = 1.0f / s;
-  uint32_t w[2] = {0, 0};
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    // The fp32 quotient.  bf16: by the reciprocal and one correction, which is exact where the quotient has few bits, as at a tie; any
-    // other quotient of two numbers of 8 bits is 2^-9 or more away from a tie.
-    const float q = v[e] * inv;
-    const float c = BF ? fmaf(fmaf(-q, s, v[e]), inv, q) : v[e] / s;
-    const int code = finite ? (int)rintf(c) : 0;
-    w[e >> 2] |= ((uint32_t)code & 0xffu) << (8 * (e & 3));
+  for (int i = 0; i < kCkptSteps; ++i) {               // (what is not there repeats the last values)
+    const CkptPlace p = ckpt_place(T, d, groups, i);
+    raw[i].fetch(X, min(p.row, T - 1) * d + min(p.col, d - 8));
   }
-  if (p.on) *reinterpret_cast<u32x2*>(codes + p.row * d + p.col) = u32x2{w[0], w[1]};
-  if (p.row < T && (threadIdx.x & 15) == 0)
-    scales[p.group] = finite ? (uint16_t)(__builtin_bit_cast(uint32_t, s) >> 16) : (uint16_t)0x7fc0;
+#pragma unroll
+  for (int i = 0; i < kCkptSteps; ++i) {
+    const CkptPlace p = ckpt_place(T, d, groups, i);
+    float v[8];
+    raw[i].get(v);
+    // the largest magnitude as an integer: infinities and NaN are the largest of all
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+    if (!p.on) top = 0;
+    top = max_dpp<0xB1>(top);
+    top = max_dpp<0x4E>(top);
+    top = max_dpp<0x141>(top);
+    top = max_dpp<0x140>(top);
+    const float amax = __builtin_bit_cast(float, top);
+    const bool finite = top < 0x7f000000u;             // below 2^127: 127 s, rounded, stays finite
+    auto up = [](float x) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) + 0xffffu) & 0xffff0000u); };
+    float s = up(amax / 127.0f);
+    if (127.0f * s < amax) s = up(s * (1.0f + 0x1p-12f));  // (127 s is exact: the quotient had been rounded down onto the grid)
+    s = fmaxf(s, 0x1p-100f);
+    const float inv = 1.0f / s;
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // The fp32 quotient.  bf16: by the reciprocal and one correction, which is exact where the quotient has few bits, as at a tie;
+      // any other quotient of two numbers of 8 bits is 2^-9 or more away from a tie.
+      const float q = v[e] * inv;
+      const float c = BF ? fmaf(fmaf(-q, s, v[e]), inv, q) : v[e] / s;
+      const int code = finite ? (int)rintf(c) : 0;
+      w[e >> 2] |= ((uint32_t)code & 0xffu) << (8 * (e & 3));
+    }
+    if (p.on) *reinterpret_cast<u32x2*>(codes + p.row * d + p.col) = u32x2{w[0], w[1]};
+    if (p.row < T && (threadIdx.x & 15) == 0)
+      scales[p.group] = finite ? (uint16_t)(__builtin_bit_cast(uint32_t, s) >> 16) : (uint16_t)0x7fc0;
+  }
 }
 
 template <bool BF>
 __global__ void __launch_bounds__(256) ckpt_unpack_kernel(const uint8_t* __restrict__ codes, const uint16_t* __restrict__ scales, int64_t T,
                                                           int d, int groups, void* __restrict__ X) {
-  const CkptPlace p = ckpt_place(T, d, groups);
-  if (!p.on) return;
-  const u32x2 w = *reinterpret_cast<const u32x2*>(codes + p.row * d + p.col);
-  const float s = bf16_float(scales[p.group]);
-  float v[8];
+  u32x2 w[kCkptSteps];
+  uint16_t sc[kCkptSteps];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3))) * s;
-  store8<BF>(X, p.row * d + p.col, v);
+  for (int i = 0; i < kCkptSteps; ++i) {
+    const CkptPlace p = ckpt_place(T, d, groups, i);
+    w[i] = *reinterpret_cast<const u32x2*>(codes + min(p.row, T - 1) * d + min(p.col, d - 8));
+    sc[i] = scales[min(p.group, T * groups - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < kCkptSteps; ++i) {
+    const CkptPlace p = ckpt_place(T, d, groups, i);
+    const float s = bf16_float(sc[i]);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(w[i][e >> 2] >> (8 * (e & 3))) * s;
+    if (p.on) store8<BF>(X, p.row * d + p.col, v);
+  }
 }
 
 }  // namespace
@@ -965,14 +994,14 @@ __global__ void __launch_bounds__(256) ckpt_unpack_kernel(const uint8_t* __restr
 void launch_ckpt_pack(bool bf16, const void* X, int64_t T, int d, uint8_t* codes, uint16_t* scales, hipStream_t st) {
   const int groups = (d + 127) / 128;
   if (T == 0) return;
-  const dim3 grid((unsigned)((T * groups + 15) / 16));
+  const dim3 grid((unsigned)((T * groups + kCkptGroups - 1) / kCkptGroups));
   if (bf16) hipLaunchKernelGGL(ckpt_pack_kernel<true>, grid, dim3(256), 0, st, X, T, d, groups, codes, scales);
   else      hipLaunchKernelGGL(ckpt_pack_kernel<false>, grid, dim3(256), 0, st, X, T, d, groups, codes, scales);
 }
 void launch_ckpt_unpack(bool bf16, const uint8_t* codes, const uint16_t* scales, int64_t T, int d, void* X, hipStream_t st) {
   const int groups = (d + 127) / 128;
   if (T == 0) return;
-  const dim3 grid((unsigned)((T * groups + 15) / 16));
+  const dim3 grid((unsigned)((T * groups + kCkptGroups - 1) / kCkptGroups));
   if (bf16) hipLaunchKernelGGL(ckpt_unpack_kernel<true>, grid, dim3(256), 0, st, codes, scales, T, d, groups, X);
   else      hipLaunchKernelGGL(ckpt_unpack_kernel<false>, grid, dim3(256), 0, st, codes, scales, T, d, groups, X);
 }
