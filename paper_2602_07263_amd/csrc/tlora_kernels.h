@@ -135,7 +135,7 @@ struct HeadParams {
   HeadStat* stats = nullptr;             // [max_rows, col_tiles]
   const float* factor = nullptr;         // [max_rows] what a row of E W^T is multiplied by
 };
-constexpr int kHeadMaxSplits = 16;
+constexpr int kHeadMaxSplits = 64;
 constexpr int kHeadShare = 8;            // K-steps
 constexpr size_t kHeadPartBytes = (size_t)512 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most two rounds of tiles
 // Largest logit of a row in a tile up to which exp(z) needs no reference, and from which on sums of it hold their digits.

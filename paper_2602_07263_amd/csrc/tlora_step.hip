@@ -458,10 +458,11 @@ __global__ void __launch_bounds__(256) norm_fwd_kernel(NormArgs a, NormJobs jobs
 }
 
 // Rows of at most kNormRow features stay in registers: a thread has eight neighbouring features and the workgroup as many waves as
-// the row needs.  A lane behind the row's end repeats its last features with zeros for their values.
+// the row needs.  A lane behind the row's end repeats its last features, which enter no sum.  Rows of up to twice that take two runs of
+// eight per thread, where no column sums are kept beside them.
 constexpr int kNormRow = 8192;
 constexpr int norm_bwd_row(bool bf16) { return bf16 ? kNormRow : kNormRow / 2; }      // (fp32 operands take twice the registers)
-static int norm_threads(int d) { return (d / 8 + 63) / 64 * 64; }
+static int norm_threads(int d) { return d <= kNormRow ? (d + 511) / 512 * 64 : (d + 1023) / 1024 * 64; }
 
 // Sums over the workgroup; each use between two barriers has a slot of its own.
 template <int N>
@@ -509,42 +510,61 @@ __device__ __forceinline__ void fill8(float (&x)[8], float v) {
   for (int e = 0; e < 8; ++e) x[e] = v;
 }
 
-// A row per workgroup: bound by HBM (31744 x 4096 bf16 183 us, 5.7 TB/s; read again for each sum, 256).
-template <bool BF>
+// A row per workgroup, CH runs per thread: bound by HBM (31744 x 4096 bf16 183 us, 5.7 TB/s; read again for each sum, 256).
+template <bool BF, int CH>
 __global__ void __launch_bounds__(1024) norm_fwd_row_kernel(NormArgs a, NormJobs jobs, void* __restrict__ H, void* __restrict__ Xn) {
   __shared__ float red[2][1][16];
   const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
   const int64_t row = (int64_t)(jb.row0 + (int)blockIdx.x - jb.unit0) * a.d;
-  const bool on = (int)threadIdx.x * 8 < a.d;
-  const int c = on ? (int)threadIdx.x * 8 : a.d - 8;
-  float y[8], h[8], g[8], p[8], q[8];
-  load8<BF>(a.Y, row + c, y);
-  load8_or<BF>(a.X, row + c, 0.f, h);
-  load8_or<BF>(jb.gate, c, 1.f, g);
-  load8_or<BF>(a.gamma_post, c, 1.f, p);
-  load8_or<BF>(Xn ? a.gamma_pre : nullptr, c, 0.f, q);
+  const int c0 = (int)threadIdx.x * 8, step = (int)blockDim.x * 8;
+  float y[CH][8], h[CH][8];
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    const int c = min(c0 + k * step, a.d - 8);
+    load8<BF>(a.Y, row + c, y[k]);
+    load8_or<BF>(a.X, row + c, 0.f, h[k]);
+  }
+  auto squares = [&](const float (&v)[CH][8]) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      float t = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t += v[k][e] * v[k][e];
+      s += c0 + k * step < a.d ? t : 0.f;
+    }
+    return s;
+  };
   float r1 = 1.f;
   if (a.gamma_post) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[0] += y[e] * y[e];
-    if (!on) s[0] = 0.f;
+    float s[1] = {squares(y)};
     norm_sums(s, red[0]);
     r1 = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) h[e] += a.res_scale * (g[e] * (y[e] * r1 * p[e]));
-  if (H && on) store8<BF>(H, row + c, h);
-  if (!Xn) return;
-  float s[1] = {0.f};
+  for (int k = 0; k < CH; ++k) {
+    const int c = min(c0 + k * step, a.d - 8);
+    float g[8], p[8];
+    load8_or<BF>(jb.gate, c, 1.f, g);
+    load8_or<BF>(a.gamma_post, c, 1.f, p);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s[0] += h[e] * h[e];
-  if (!on) s[0] = 0.f;
+    for (int e = 0; e < 8; ++e) h[k][e] += a.res_scale * (g[e] * (y[k][e] * r1 * p[e]));
+    if (H && c0 + k * step < a.d) store8<BF>(H, row + c, h[k]);
+  }
+  if (!Xn) return;
+  float s[1] = {squares(h)};
   norm_sums(s, red[1]);
   const float r2 = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) h[e] = h[e] * r2 * q[e];
-  if (on) store8<BF>(Xn, row + c, h);
+  for (int k = 0; k < CH; ++k) {
+    const int c = c0 + k * step;
+    if (c >= a.d) continue;
+    float q[8];
+    load8<BF>(a.gamma_pre, c, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[k][e] = h[k][e] * r2 * q[e];
+    store8<BF>(Xn, row + c, h[k]);
+  }
 }
 
 // 1 / sqrt(x): the instruction's estimate and one Newton step (which has no say about 0 and infinity)
@@ -675,12 +695,90 @@ __global__ void __launch_bounds__(norm_bwd_row(BF) / 8) norm_bwd_unit_kernel(Nor
   }
 }
 
-// ---- wider rows: read again for every sum -----------------------------------------------------------------------------------
 // rstd of Y and of H, and the factor of H in D = dH + r2 (dXn gamma_pre) - H k2
 struct NormRow {
   float r1, r2, k2, pad;
 };
 
+// Backward of one row per workgroup, two runs per thread; the column sums are left to norm_bwd_cols_kernel.
+template <bool BF>
+__global__ void __launch_bounds__(1024) norm_bwd_row_kernel(NormArgs a, NormJobs jobs, NormGrads g, NormRow* __restrict__ rows) {
+  __shared__ float red[2][5][16];
+  const NormJob jb = jobs.job[norm_job(jobs, blockIdx.x)];
+  const int t = jb.row0 + (int)blockIdx.x - jb.unit0;
+  const int64_t row = (int64_t)t * a.d;
+  const int c0 = (int)threadIdx.x * 8, step = (int)blockDim.x * 8;
+  const float inv_d = 1.0f / (float)a.d;
+  float y[2][8], h[2][8], D[2][8], gq[2][8];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = min(c0 + k * step, a.d - 8);
+    load8<BF>(a.Y, row + c, y[k]);
+    load8_or<BF>(a.X, row + c, 0.f, h[k]);
+    load8_or<BF>(g.dH, row + c, 0.f, D[k]);
+    load8_or<BF>(g.dXn, row + c, 0.f, gq[k]);
+  }
+  float r1 = 1.f;
+  if (a.gamma_post) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] += c0 + k * step < a.d ? y[k][e] * y[k][e] : 0.f;
+    norm_sums(s, red[0]);
+    r1 = rstd_of(s[0] * inv_d + a.eps);
+  }
+  float s[5] = {};                          // as norm_bwd_unit_kernel's
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = min(c0 + k * step, a.d - 8);
+    float agp[8], p[8], q[8];
+    load8_or<BF>(jb.gate, c, 1.f, agp);
+    load8_or<BF>(a.gamma_post, c, 1.f, p);
+    load8_or<BF>(g.dXn ? a.gamma_pre : nullptr, c, 0.f, q);
+    const bool on = c0 + k * step < a.d;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      agp[e] *= p[e] * a.res_scale;
+      const float w = agp[e] * y[k][e];
+      h[k][e] += w * r1;
+      gq[k][e] *= q[e];
+      if (on) {
+        s[0] += h[k][e] * h[k][e];
+        s[1] += gq[k][e] * h[k][e];
+        s[2] += D[k][e] * w;
+        s[3] += gq[k][e] * w;
+        s[4] += h[k][e] * w;
+      }
+    }
+  }
+  norm_sums(s, red[1]);
+  float r2 = 0.f, k2 = 0.f;
+  if (g.dXn) {
+    r2 = rstd_of(s[0] * inv_d + a.eps);
+    k2 = s[1] * r2 * r2 * r2 * inv_d;
+  }
+  const float k1 = a.gamma_post ? (s[2] + r2 * s[3] - k2 * s[4]) * r1 * r1 * r1 * inv_d : 0.f;
+  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, k2, 0.f};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = c0 + k * step;
+    if (c >= a.d) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) D[k][e] += r2 * gq[k][e] - h[k][e] * k2;
+    if (g.dX) store8<BF>(g.dX, row + c, D[k]);
+    if (g.dY) {
+      float agp[8], p[8];
+      load8_or<BF>(jb.gate, c, 1.f, agp);
+      load8_or<BF>(a.gamma_post, c, 1.f, p);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D[k][e] = r1 * (agp[e] * (p[e] * a.res_scale) * D[k][e]) - y[k][e] * k1;
+      store8<BF>(g.dY, row + c, D[k]);
+    }
+  }
+}
+
+// ---- wider rows: read again for every sum -----------------------------------------------------------------------------------
 template <bool BF>
 __device__ __forceinline__ void norm_elements(const NormArgs& a, const void* gate, const NormGrads& g, int64_t row, int c, float r1, float r2,
                                               float k2, float (&y)[8], float (&pn)[8], float (&h)[8], float (&gn)[8], float (&D)[8],
@@ -840,10 +938,16 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* __restri
 
 void launch_norm_fwd(bool bf16, const NormArgs& a, const NormJobs& jobs, int rows, void* H, void* Xn, hipStream_t st) {
   if (rows == 0) return;
-  if (a.d <= kNormRow) {
+  if (a.d <= 2 * kNormRow) {
     const dim3 block(norm_threads(a.d));
-    if (bf16) hipLaunchKernelGGL(norm_fwd_row_kernel<true>, dim3(rows), block, 0, st, a, jobs, H, Xn);
-    else      hipLaunchKernelGGL(norm_fwd_row_kernel<false>, dim3(rows), block, 0, st, a, jobs, H, Xn);
+#define TLORA_NORM_FWD(CH)                                                                                            \
+  do {                                                                                                               \
+    if (bf16) hipLaunchKernelGGL((norm_fwd_row_kernel<true, CH>), dim3(rows), block, 0, st, a, jobs, H, Xn);          \
+    else      hipLaunchKernelGGL((norm_fwd_row_kernel<false, CH>), dim3(rows), block, 0, st, a, jobs, H, Xn);         \
+  } while (0)
+    if (a.d <= kNormRow) TLORA_NORM_FWD(1);
+    else                 TLORA_NORM_FWD(2);
+#undef TLORA_NORM_FWD
     return;
   }
   if (bf16) hipLaunchKernelGGL(norm_fwd_kernel<true>, dim3(rows), dim3(256), 0, st, a, jobs, H, Xn);
@@ -872,6 +976,12 @@ void launch_norm_bwd_rows(bool bf16, const NormArgs& a, const NormJobs& jobs, co
                           hipStream_t st) {
   if (rows == 0) return;
   NormRow* const r = reinterpret_cast<NormRow*>(row_stats);
+  if (a.d <= 2 * kNormRow) {
+    const dim3 block((a.d + 1023) / 1024 * 64);      // (fp32 rows from kNormRow / 2 on too)
+    if (bf16) hipLaunchKernelGGL(norm_bwd_row_kernel<true>, dim3(rows), block, 0, st, a, jobs, g, r);
+    else      hipLaunchKernelGGL(norm_bwd_row_kernel<false>, dim3(rows), block, 0, st, a, jobs, g, r);
+    return;
+  }
   if (bf16) hipLaunchKernelGGL(norm_bwd_rows_kernel<true>, dim3(rows), dim3(256), 0, st, a, jobs, g, r);
   else      hipLaunchKernelGGL(norm_bwd_rows_kernel<false>, dim3(rows), dim3(256), 0, st, a, jobs, g, r);
 }

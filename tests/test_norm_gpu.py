@@ -50,7 +50,7 @@ def _nan_like(t, n=None, f32=False):
 # dtype, d, tokens: one token, odd feature sizes, jobs without tokens, widths beyond every register variant
 CASES = [("bf16", 8, [1]), ("bf16", 4096, [5, 1, 7]), ("bf16", 1544, [33, 0, 68]), ("f32", 264, [100, 29]), ("bf16", 256, [700, 1, 0, 323]),
          ("bf16", 8200, [9, 4]), ("f32", 4096, [17, 40]), ("bf16", 17408, [3, 6]), ("bf16", 5120, [1030, 70]),
-         ("bf16", 8192, [5]), ("f32", 4104, [6, 3])]
+         ("bf16", 8192, [5]), ("f32", 4104, [6, 3]), ("bf16", 16384, [3, 2]), ("f32", 16392, [4])]
 
 
 @pytest.mark.parametrize("post,pre,gates,X", [(1, 1, 1, 1), (0, 1, 0, 1), (1, 0, 1, 1), (0, 1, 0, 0), (1, 1, 0, 0)],
