@@ -371,7 +371,8 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  *     z_t = H_t . W;   lse_t = log sum_v exp(z_tv);   loss_t = lse_t - z_t,y(t)
  *     job_loss_j = sum_{t of job j} w_t loss_t / sum_{t of job j} w_t
  * targets (DEVICE int32 [T]) outside [0, vocab) mark tokens without a loss (prompts, padding): their loss, lse and dH rows are
- * zero, whatever their H row holds, and they enter no sum.  weights (DEVICE fp32 [T], finite; NULL = ones).  A job whose
+ * zero, whatever their H row holds, and they enter no sum.  weights (DEVICE fp32 [T], finite; NULL = ones); a
+ * token of weight 0 has a loss, but neither that nor its H row enters a mean or a gradient (dH row zero).  A job whose
  * weights sum to zero has job_loss 0 and no gradient.
  * tlora_ce_fwd_bwd also makes  dH_t = g_t (softmax(z_t) - onehot(y_t)) . W^T  with g_t = dloss[t] (DEVICE fp32 [T]) or, with
  * dloss NULL, of L = sum_j job_loss_j.  W is frozen: no gradient.

@@ -156,7 +156,7 @@ __device__ __forceinline__ void ce_job(const CeTokens& c, int j, int threads, fl
     if (ce_live(c.targets[t], c.vocab)) {
       const double v = c.weights ? (double)c.weights[t] : 1.0;
       w += v;
-      s += v * (double)c.token_loss[t];
+      if (v != 0.0) s += v * (double)c.token_loss[t];   // (whatever the loss of a token without weight is)
     }
   w = sums(w);
   s = sums(s);
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
     if (lse) lse[t] = l;
   }
   if (!GRAD) return;
-  const float rho = l >= -20.f && l <= 80.f ? 0.f : l;
+  const float rho = l >= -20.f && l <= 60.f ? 0.f : l;     // (share * exp(-60) is still an ordinary number)
   uint16_t* const row = E + (int64_t)r * h.ld;
   const int n8 = (h.vocab + 7) & ~7;
   if (!plain || rho != 0.f)
@@ -338,7 +338,8 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
   }
   if (lane == 0) {
     row[y] = at_y;
-    factor[r] = c.share[t] * expf(rho - l);
+    const float g = c.share[t];
+    factor[r] = g == 0.f ? 0.f : g * expf(rho - l);     // (0: a row of zeros, whatever the exponentials are)
   }
 }
 

@@ -120,8 +120,8 @@ def test_loss_and_gradient_match_the_oracle(tokens, d, V, ld, weighted):
         assert torch.equal(a, b)                # the same statistics, the same bits
 
 
-@pytest.mark.parametrize("std,shift", [(40.0, 0.0), (2.0, 200.0), (2.0, -200.0), (30.0, -60.0), (0.0, 0.0)],
-                         ids=["wide", "high", "low", "mixed", "equal"])
+@pytest.mark.parametrize("std,shift", [(40.0, 0.0), (2.0, 200.0), (2.0, -200.0), (30.0, -60.0), (0.0, 0.0), (3.0, 56.0), (3.0, -36.0)],
+                         ids=["wide", "high", "low", "mixed", "equal", "at_the_top", "at_the_bottom"])
 def test_logits_far_from_zero(std, shift):
     """Rows whose exponentials need references of their own: logits of hundreds, of either sign, and all equal."""
     import torch
@@ -188,6 +188,24 @@ def test_infinite_and_nan_rows_stay_their_own():
     for s, t in ((a[0], b[0]), (a[1], b[1]), (a[3], b[3])):
         assert torch.equal(s[keep], t[keep])
     assert torch.isnan(b[0][5]) and torch.isnan(b[3][5]).all() and torch.isnan(b[2][0])
+
+
+def test_tokens_of_weight_zero_enter_nothing():
+    import torch
+    off = [0, 25, 60]
+    H, W, y = _inputs(22, 60, 64, 300, 304, ignored=0.0)
+    w = np.random.default_rng(1).uniform(0.5, 2.0, 60).astype(np.float32)
+    w[[3, 30, 59]] = 0.0
+    r = _oracle(H, W, y, 300, off, w)
+    H[3], H[59, 7] = np.nan, np.inf
+    head = _head(H, W, y, 300, off, w)
+    loss, lse, job, dH = _outs(head)
+    head.fwd_bwd(loss, lse, job, dH)
+    torch.cuda.synchronize()
+    assert not torch.isfinite(loss[[3, 59]]).any() and not dH[[3, 30, 59]].any()
+    loss[[3, 59]] = torch.from_numpy(r["loss"][[3, 59]]).float().cuda()      # (for the comparison of the rest)
+    lse[[3, 59]] = torch.from_numpy(r["lse"][[3, 59]]).float().cuda()
+    _check((loss, lse, job, dH), r, np.nan_to_num(H, nan=0.0, posinf=0.0), W, y, 300)
 
 
 def test_pieces_of_a_long_batch():
