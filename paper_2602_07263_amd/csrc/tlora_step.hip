@@ -38,7 +38,7 @@ __device__ __forceinline__ double block_sum_1024(double x, double* red) {
 // what each of its tokens' losses counts for (dloss, or weight / sum).  Tokens without a loss get zeros.  Of the workgroups behind
 // those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the batch is one
 // piece moves the others' rows of H to their places, for which it counts the list up to its tokens itself (16 KB of targets at
-// most, from the L2; a launch of its own that reads the list costs 6 us); the last copy the end of W.
+// most, from the L2; a launch of its own that reads the list would cost more); the last copy the end of W.
 // ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ bool ce_live(int y, int vocab) { return (unsigned)y < (unsigned)vocab; }
 
@@ -511,7 +511,7 @@ __device__ __forceinline__ void fill8(float (&x)[8], float v) {
   for (int e = 0; e < 8; ++e) x[e] = v;
 }
 
-// A row per workgroup, CH runs per thread: bound by HBM (31744 x 4096 bf16 183 us, 5.7 TB/s; read again for each sum, 256).
+// A row per workgroup, CH runs per thread: bound by HBM (31744 x 4096 bf16 193 us, 5.4 TB/s; read again for each sum, 256).
 template <bool BF, int CH>
 __global__ void __launch_bounds__(1024) norm_fwd_row_kernel(NormArgs a, NormJobs jobs, void* __restrict__ H, void* __restrict__ Xn) {
   __shared__ float red[2][1][16];
@@ -580,8 +580,7 @@ __device__ __forceinline__ float rstd_of(float x) {
 // for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
 // what the second sums give, D = dH + r2 (dXn gamma_pre) - k2 H, so the last sum is put together from three that need rstd_Y
 // alone; and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
-// barrier.  31744 x 4096 bf16 with all sums 316 us
-// (5.1 TB/s with the partial sums).
+// barrier.  31744 x 4096 bf16 with all sums 320 us (4.9 TB/s).
 // BOTH: dX and dY are wanted.  Every lane then stores without a condition -- those behind the row's end its last features once more,
 // the same values -- since behind a store that may not have been issued the compiler waits for all those that may.
 template <bool BF, bool SUMS, bool BOTH>
@@ -1003,7 +1002,7 @@ void launch_norm_reduce(const float* partial, const NormJobs& jobs, int first_ve
 
 // ---------------------------------------------------------------------------------------------------
 // Activations in 8 bits: 16 lanes of 8 values have a group of 128; a thread has four groups' values in flight.  Bound by memory (31744 x
-// 12288 bf16: packing 230 us, 5.1 TB/s, unpacking 193 us, 6.1 TB/s; one group at a time and the maximum by exchanges through LDS, 259
+// 12288 bf16: packing 219 to 245 us, 4.8 to 5.4 TB/s, unpacking 193 us, 6.1 TB/s; one group at a time and the maximum by exchanges through LDS, 259
 // and 197).
 // ---------------------------------------------------------------------------------------------------
 namespace {
