@@ -2148,7 +2148,9 @@ NormArgs norm_args(const tlora_norm_t* p) {
   return a;
 }
 // Calls launch(jobs, rows, units) for group after group of jobs that have tokens (with `idle`: of all jobs).  Without gates all
-// tokens are one job.  unit_rows 1: units are rows.
+// tokens are one job.  unit_rows 1: units are rows, and a job's are spread over launches, since a launch has less than 2^32 threads
+// and a row takes up to 1024 of them.
+constexpr int32_t kNormLaunchRows = 1 << 21;
 template <class Launch>
 void norm_groups(const tlora_norm_t* p, const NormPlan& N, int unit_rows, float* const* dgates, bool idle, const Launch& launch) {
   NormJobs jobs;
@@ -2162,18 +2164,23 @@ void norm_groups(const tlora_norm_t* p, const NormPlan& N, int unit_rows, float*
   };
   const int J = N.by_job ? p->num_jobs : 1;
   for (int j = 0; j < J; ++j) {
-    NormJob jb;
-    jb.row0 = (int32_t)(N.by_job ? p->offsets[j] : 0);
-    jb.row1 = (int32_t)(N.by_job ? p->offsets[j + 1] : N.T);
-    if (jb.row1 == jb.row0 && !idle) continue;
-    jb.gate = N.by_job ? p->gates[j] : nullptr;
-    jb.dgate = dgates ? dgates[j] : nullptr;
-    jb.unit0 = units;
-    jb.units = (jb.row1 - jb.row0 + unit_rows - 1) / unit_rows;
-    rows += jb.row1 - jb.row0;
-    units += jb.units;
-    jobs.job[jobs.n++] = jb;
-    if (jobs.n == kNormJobs) flush();
+    int32_t at = (int32_t)(N.by_job ? p->offsets[j] : 0);
+    const int32_t end = (int32_t)(N.by_job ? p->offsets[j + 1] : N.T);
+    if (at == end && !idle) continue;
+    do {
+      NormJob jb;
+      jb.row0 = at;
+      jb.row1 = unit_rows == 1 ? std::min(end, at + (kNormLaunchRows - rows)) : end;
+      jb.gate = N.by_job ? p->gates[j] : nullptr;
+      jb.dgate = dgates ? dgates[j] : nullptr;
+      jb.unit0 = units;
+      jb.units = (jb.row1 - jb.row0 + unit_rows - 1) / unit_rows;
+      rows += jb.row1 - jb.row0;
+      units += jb.units;
+      jobs.job[jobs.n++] = jb;
+      at = jb.row1;
+      if (jobs.n == kNormJobs || (unit_rows == 1 && rows == kNormLaunchRows)) flush();
+    } while (at < end);
   }
   flush();
 }

@@ -88,3 +88,27 @@ def test_loss():
     assert torch.equal(job[1:], j)
     for a in range(0, T - LAST, 200_000):
         assert not dH[a:min(a + 200_000, T - LAST)].any()
+
+
+def test_norm_of_more_rows_than_a_launch_takes():
+    # 2^22 rows of 1024 threads are 2^32 threads.  Rows of a few kinds, other ones in the second half; one row's result does not
+    # depend on where it lies.
+    import torch
+    from paper_2602_07263_amd import tlora
+    rows, d, bf = 1 << 22, 8192, torch.bfloat16
+    torch.cuda.empty_cache()
+    kinds = _fill(torch.empty(16, d, dtype=bf, device="cuda"), 5)
+    gamma = torch.ones(d, dtype=bf, device="cuda") * 1.25
+    few = torch.empty_like(kinds)
+    tlora.ResidualNorm("bf16", [0, 16], None, kinds, gamma, 1e-5).fwd(None, few)
+    Y, Xn = torch.empty(rows, d, dtype=bf, device="cuda"), torch.empty(rows, d, dtype=bf, device="cuda")
+    for h in range(2):
+        Y[h * rows // 2:(h + 1) * rows // 2].view(-1, 8, d).copy_(kinds[8 * h:8 * h + 8])
+    Xn.fill_(float("nan"))
+    print("norm forward, 2^22 rows", flush=True)
+    tlora.ResidualNorm("bf16", [0, rows], None, Y, gamma, 1e-5).fwd(None, Xn)
+    torch.cuda.synchronize()
+    for h in range(2):
+        got = Xn[h * rows // 2:(h + 1) * rows // 2].view(-1, 8, d)
+        for a in range(0, got.shape[0], 1 << 14):
+            assert torch.equal(got[a:a + (1 << 14)], few[8 * h:8 * h + 8].expand(1 << 14, 8, d)), (h, a)
