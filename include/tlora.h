@@ -347,6 +347,8 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
  * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs
  * gamma_post (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or added to with TLORA_BWD_ACCUMULATE (the only flag);
  * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap no inputs.
+ * mean(V^2) + eps of a row is to lie between 2^-80 and 2^80: its powers are fp32 numbers, and outside (a row of zeros with eps 0, say)
+ * that row, and the sums it enters, may be infinite or not a number.
  * tlora_norm_fwd needs no workspace.  tlora_norm_bwd's: 256-byte aligned, tlora_norm_workspace_bytes.  Neither call allocates,
  * copies or synchronises, so both may be captured into a graph. */
 typedef struct {
@@ -380,7 +382,7 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  * products (half a step of a bf16 number off, as the probabilities of tlora_attention_*); logits are never stored.  Logits, sums and
  * statistics are fp32.  loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
  * bf16 only (TLORA_EDTYPE otherwise); d_model a multiple of 8; vocab >= 1, of any size; ld_w a multiple of 8, vocab <= ld_w <=
- * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned.
+ * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned; outputs overlap no inputs.
  * The workspace depends on num_jobs, T, d_model, vocab, ld_w and with_grad (0: tlora_ce_fwd, else either call), and never
  * falls when tokens are added.  Neither call allocates, copies or synchronises, so both may be captured into a graph. */
 typedef struct {
@@ -406,8 +408,8 @@ int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float
  * tensor's dtype: |x^ - x| <= s / 2 and that rounding.  A group with a value that is infinite, not a number, or 2^127 or larger comes
  * back as NaN.
  * packed: DEVICE, 256-byte aligned, tlora_ckpt_bytes(T, d): int8 [T, d], then, from the next multiple of 256 bytes on, the scales,
- * bf16 [T, ceil(d / TLORA_CKPT_GROUP)].  d a multiple of 8 and at most TLORA_MAX_FEATURES, 0 <= T <= TLORA_MAX_TOKENS; X: DEVICE
- * [T, d] of `dtype`, 16-byte aligned.
+ * bf16 [T, ceil(d / TLORA_CKPT_GROUP)].  d a multiple of 8 and at most TLORA_MAX_FEATURES, 0 <= T <= TLORA_MAX_TOKENS, fewer than 2^30
+ * groups in all (TLORA_EINVAL otherwise); X: DEVICE [T, d] of `dtype`, 16-byte aligned.
  * tlora_bwd_ckpt is tlora_bwd of the problem whose X are the packed values x^: p->X is not read and may be NULL.  With
  * TLORA_BWD_REUSE_S the S_j of the tlora_fwd before it on this workspace are taken (made from the X that the forward had), otherwise
  * S_j = X^_j.A_j.  Its workspace, tlora_ckpt_workspace_bytes, begins with that of tlora_fwd / tlora_bwd of the problem; flags and

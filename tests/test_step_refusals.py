@@ -170,3 +170,12 @@ def test_holders_refuse_tensors_of_another_layout_or_type():
         tlora.ResidualNorm("bf16", [0, 4], H, H, None, 1e-5, gates=[torch.zeros(16)])
     with pytest.raises(tlora.TloraError, match="Checkpoint"):
         tlora.Checkpoint("bf16", 4, 16, "cpu").pack(H.t())
+
+
+def test_eight_bits_refuse_more_groups_than_a_launch_takes():
+    L = tlora.lib()
+    for T, d, ok in (((1 << 23) - 1, 128 * 128, True), (1 << 23, 128 * 128, False), (1 << 24, 63 * 128, True), (1 << 24, 63 * 128 + 8, False)):
+        assert (L.tlora_ckpt_bytes(T, d) > 0) == ok
+        if not ok:
+            assert L.tlora_ckpt_pack(1, P(0x1000), T, d, P(WS), None) == -1
+            assert L.tlora_ckpt_unpack(1, P(WS), T, d, P(0x1000), None) == -1
