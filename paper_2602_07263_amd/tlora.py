@@ -560,6 +560,8 @@ class LayerProblem:
 
     def bwd_ckpt(self, packed, dY, dX, dA, dB, reuse_S: bool = False, flags: int = 0) -> None:
         """bwd from the 8-bit form of X (`packed`: the bytes of Checkpoint.pack); bwd_ckpt_workspace comes first."""
+        if packed is not None and packed.numel() * packed.element_size() < int(lib().tlora_ckpt_bytes(self.T, self.d_in)):
+            raise TloraError("bwd_ckpt: packed has fewer bytes than X's 8-bit form")
         c_dA, c_dB = _grad_ptr_arrays(len(self.ranks), None if dA is None else [a.data_ptr() if a.numel() else 0 for a in dA],
                                       None if dB is None else [b.data_ptr() if b.numel() else 0 for b in dB])
         _check(lib().tlora_bwd_ckpt(ctypes.byref(self.prob), _ptr(packed), _ptr(dY), _ptr(dX), c_dA, c_dB,
@@ -820,6 +822,12 @@ class DecoderLayer:
                                      ctypes.c_void_p(self._stream())), "tlora_layer_bwd")
 
 
+def _holds(ok: bool, what: str) -> None:
+    """A holder's tensors have to have what its offsets and sizes say: the C call takes addresses and cannot know."""
+    if not ok:
+        raise TloraError(what)
+
+
 class ResidualNorm:
     """Residual stream and norms between two blocks (argument marshalling for tlora_norm_fwd / tlora_norm_bwd).
     gamma_post, gamma_pre, X, gates (a list of one [d_model] tensor or None per job) may be None, as the C call has it."""
@@ -834,6 +842,12 @@ class ResidualNorm:
         vectors = {f"gates[{j}]": g for j, g in enumerate(gates or [])}
         tensors = dict(X=X, Y=Y, gamma_pre=gamma_pre, gamma_post=gamma_post, **vectors)
         _dense(tensors, dict.fromkeys(tensors, torch.bfloat16 if dtype == "bf16" else torch.float32), "ResidualNorm")
+        for name, t in dict(X=X, Y=Y).items():
+            _holds(t is None or (t.dim() == 2 and t.shape[1] == self.d and t.shape[0] >= self.offsets[-1]),
+                   f"ResidualNorm: {name} must be [{self.offsets[-1]} or more, {self.d}]")
+        _holds(gates is None or len(gates) == J, "ResidualNorm: one gate (or None) per job")
+        for name, t in dict(gamma_pre=gamma_pre, gamma_post=gamma_post, **vectors).items():
+            _holds(t is None or t.numel() == self.d, f"ResidualNorm: {name} must have {self.d} elements")
         self._gates = None if gates is None else (ctypes.c_void_p * J)(*[_ptr(g) for g in gates])
         self._keep = [X, Y, gamma_pre, gamma_post, gates]
         self.prob = tlora_norm_t(TLORA_BF16 if dtype == "bf16" else TLORA_F32, J, self.d, self._off, float(eps), float(res_scale),
@@ -870,6 +884,10 @@ class LossHead:
         self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
         _dense(dict(H=H, W=W, targets=targets, weights=weights),
                dict(H=torch.bfloat16, W=torch.bfloat16, targets=torch.int32, weights=torch.float32), "LossHead")
+        T, d = self.offsets[-1], int(W.shape[0])
+        _holds(H is None or (H.dim() == 2 and H.shape[1] == d and H.shape[0] >= T), f"LossHead: H must be [{T} or more, {d}]")
+        for name, t in dict(targets=targets, weights=weights).items():
+            _holds(t is None or t.numel() >= T, f"LossHead: {name} must have {T} elements or more")
         self._keep = [H, W, targets, weights]
         self.prob = tlora_ce_t(TLORA_BF16, J, int(W.shape[0]), int(vocab), int(W.shape[1]), self._off, _ptr(H), _ptr(W),
                                _ptr(targets), _ptr(weights))

@@ -179,3 +179,24 @@ def test_eight_bits_refuse_more_groups_than_a_launch_takes():
         if not ok:
             assert L.tlora_ckpt_pack(1, P(0x1000), T, d, P(WS), None) == -1
             assert L.tlora_ckpt_unpack(1, P(WS), T, d, P(0x1000), None) == -1
+
+
+def test_holders_refuse_tensors_smaller_than_their_offsets_say():
+    import torch
+    bf = torch.bfloat16
+    z = lambda *n: torch.zeros(*n, dtype=bf)
+    y = torch.zeros(4, dtype=torch.int32)
+    tlora.LossHead([0, 1, 4], z(5, 16), z(16, 24), 20, y, weights=torch.zeros(4))
+    for args, w in (((z(3, 16), z(16, 24), y), None), ((z(4, 8), z(16, 24), y), None), ((z(4, 16), z(16, 24), y[:3]), None),
+                    ((z(4, 16), z(16, 24), y), torch.zeros(3)), ((z(64), z(16, 24), y), None)):
+        with pytest.raises(tlora.TloraError, match="LossHead"):
+            tlora.LossHead([0, 1, 4], args[0], args[1], 20, args[2], weights=w)
+    mk = lambda X=z(4, 16), Y=z(4, 16), pre=z(16), **k: tlora.ResidualNorm("bf16", [0, 1, 4], X, Y, pre, 1e-5, **k)
+    mk(gates=[None, z(16)], gamma_post=z(16))
+    for kw in (dict(X=z(3, 16)), dict(X=z(4, 24)), dict(Y=z(3, 16)), dict(pre=z(8)), dict(gamma_post=z(24)), dict(gates=[z(16)]),
+               dict(gates=[z(16)] * 3), dict(gates=[None, z(8)])):
+        with pytest.raises(tlora.TloraError, match="ResidualNorm"):
+            mk(**kw)
+    layer = tlora.LayerProblem("bf16", 16, 16, [4], [0, 4], [1.0], z(4, 16), z(16, 16), [z(16, 4)], [z(4, 16)])
+    with pytest.raises(tlora.TloraError, match="packed"):
+        layer.bwd_ckpt(torch.zeros(255, dtype=torch.uint8), z(4, 16), None, None, None)
