@@ -218,3 +218,34 @@ def test_replays_from_a_captured_stream():
         torch.cuda.synchronize()
         for a, b in zip(out, ref):
             assert torch.equal(a, b)
+
+
+def test_holders_use_the_current_stream():
+    # behind a long product on a side stream: a call on any other stream would read Y before it is written
+    import torch
+    from paper_2602_07263_amd import tlora
+    bf, side = torch.bfloat16, torch.cuda.Stream()
+    v = _draw(9, "bf16", 64, 512, 1)
+    n = _norm(v, "bf16", [0, 64], 1.0)
+    Y = n._keep[1]
+    want, got = _nan_like(Y), _nan_like(Y)
+    n.fwd(want, None)
+    saved = Y.clone()
+    Y.zero_()
+    big = torch.randn(8192, 8192, device="cuda").to(bf)
+    packed = tlora.Checkpoint("bf16", 64, 512, "cuda")
+    back = _nan_like(Y)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        assert tlora._current_stream(torch) == side.cuda_stream == torch.cuda.current_stream().cuda_stream
+        for _ in range(3):
+            big @ big
+        Y.copy_(saved)
+        n.fwd(got, None)
+        packed.pack(Y)
+        packed.unpack(back)
+    assert tlora._current_stream(torch) == torch.cuda.current_stream().cuda_stream != side.cuda_stream
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    # a code is half a step off at most, and a value of bf16 half a step of its own
+    assert torch.all((back - saved).float().abs() <= saved.float().abs().amax() * (1.01 / 254 + 2 ** -8))
