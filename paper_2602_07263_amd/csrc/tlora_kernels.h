@@ -199,6 +199,7 @@ struct NormArgs {
 struct NormGrads {
   const void *dH = nullptr, *dXn = nullptr;
   void *dX = nullptr, *dY = nullptr;
+  int sums = 0;                            // column sums that are wanted: 1 dgamma_post, 2 dgamma_pre, 4 dgates
 };
 struct NormJob {
   int32_t row0 = 0, row1 = 0;

@@ -576,7 +576,7 @@ __device__ __forceinline__ float rstd_of(float x) {
 }
 
 // Backward of a unit's rows, one after the other; with SUMS the unit's column sums stay in registers and leave as partial
-// [unit][3][d] (dgamma_post, dgamma_pre, dgate).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
+// [unit][3][d] (dgamma_post, dgamma_pre, dgate; those that are wanted).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
 // for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
 // what the second sums give, D = dH + r2 (dXn gamma_pre) - k2 H, so the last sum is put together from three that need rstd_Y
 // alone; and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
@@ -687,11 +687,11 @@ __global__ void __launch_bounds__(norm_bwd_row(BF) / 8) norm_bwd_unit_kernel(Nor
     load8_or<BF>(a.gamma_post, c, 1.f, p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = gate[e] * a.res_scale * sum_y[e];
-    store8<false>(o, 0, v);
-    store8<false>(o, a.d, sum_h);
+    if (g.sums & 1) store8<false>(o, 0, v);
+    if (g.sums & 2) store8<false>(o, a.d, sum_h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = p[e] * a.res_scale * sum_y[e];
-    store8<false>(o, 2 * (int64_t)a.d, v);
+    if (g.sums & 4) store8<false>(o, 2 * (int64_t)a.d, v);
   }
 }
 
@@ -889,7 +889,7 @@ __global__ void __launch_bounds__(256) norm_bwd_cols_kernel(NormArgs a, NormJobs
   __syncthreads();
   for (int i = threadIdx.x; i < 3 * 512; i += 256) {
     const int k = i >> 9, x = i & 511, col = (int)blockIdx.y * 512 + x;
-    if (col < a.d)
+    if (col < a.d && (g.sums >> k & 1))
       partial[((int64_t)(jobs.unit_base + (int)blockIdx.x) * 3 + k) * a.d + col] =
           (red[0][k][x] + red[1][k][x]) + (red[2][k][x] + red[3][k][x]);
   }
