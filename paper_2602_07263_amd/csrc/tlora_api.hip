@@ -2355,14 +2355,13 @@ int ce_run(const tlora_ce_t* p, bool grad, const float* dloss, float* loss, floa
   const bool one_piece = C.T <= kCePieceRows && C.T <= C.piece;     // (the first launch counts the list per row)
   {
     Timed t(TLORA_K_LOSS, st);
-    const std::vector<int32_t> offsets(p->offsets, p->offsets + J + 1);
     CePrepare q;
     q.dloss = dloss;  q.loss = loss;  q.lse = lse;
     q.H = H;  q.dH = static_cast<uint16_t*>(dH);
     q.rows = one_piece ? rows : nullptr;
     q.W = W;  q.ld = p->ld_w;
     q.W_tail = grad && p->vocab % 32 ? W_tail : nullptr;
-    launch_ce_prepare(c, J, offsets.data(), q, st);
+    launch_ce_prepare(c, J, p->offsets, q, st);
   }
   for (int64_t first = 0; first < C.T; first += C.piece) {
     HeadParams h;

@@ -183,7 +183,7 @@ struct CePrepare {
   int64_t ld = 0;
   uint16_t* W_tail = nullptr;
 };
-void launch_ce_prepare(const CeTokens& c, int num_jobs, const int32_t* host_offsets, const CePrepare& p, hipStream_t st);
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const int64_t* host_offsets, const CePrepare& p, hipStream_t st);
 void launch_ce_gather(const HeadParams& h, const CeTokens& c, const uint16_t* H, uint16_t* rows, int d, hipStream_t st);
 // Statistics -> losses; E null: no gradient.
 void launch_ce_finish(const HeadParams& h, const CeTokens& c, uint16_t* E, uint16_t* E_tail, float* factor, float* loss, float* lse,

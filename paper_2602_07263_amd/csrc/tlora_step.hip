@@ -345,16 +345,20 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
 
 }  // namespace
 
-void launch_ce_prepare(const CeTokens& c, int num_jobs, const int32_t* host_offsets, const CePrepare& p, hipStream_t st) {
+void launch_ce_prepare(const CeTokens& c, int num_jobs, const int64_t* host_offsets, const CePrepare& p, hipStream_t st) {
   const int row_groups = p.dH || p.rows ? (c.T + 15) / 16 : 0;
   const dim3 grid(1 + num_jobs + row_groups + (p.W_tail ? (c.d + 31) / 32 : 0));
   int32_t* const table = const_cast<int32_t*>(c.offsets);
   CeOffsets args = {};
   if (num_jobs <= kCeArgJobs) {
-    for (int j = 0; j <= num_jobs; ++j) args.at[j] = host_offsets[j];
+    for (int j = 0; j <= num_jobs; ++j) args.at[j] = (int32_t)host_offsets[j];
     hipLaunchKernelGGL(ce_prepare_kernel<true>, grid, dim3(1024), 0, st, c, num_jobs, table, args, p, row_groups);
   } else {
-    launch_table_write(host_offsets, sizeof(int32_t) * ((size_t)num_jobs + 1), table, st);
+    for (int j = 0, n; j <= num_jobs; j += n) {
+      n = std::min(num_jobs + 1 - j, kCeArgJobs);
+      for (int i = 0; i < n; ++i) args.at[i] = (int32_t)host_offsets[j + i];
+      launch_table_write(args.at, sizeof(int32_t) * (size_t)n, table + j, st);
+    }
     hipLaunchKernelGGL(ce_prepare_kernel<false>, grid, dim3(1024), 0, st, c, num_jobs, table, args, p, row_groups);
   }
 }
