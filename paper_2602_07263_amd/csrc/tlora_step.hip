@@ -273,6 +273,11 @@ __global__ void __launch_bounds__(256) head_grad_reduce_kernel(const float* __re
 // relative to one reference rho, the target's less the sum itself, and factor = share * exp(rho - lse).  rho is 0 unless the sum
 // itself is out of range for it, so that as a rule (logits within head_reference's bounds) one element of the row is touched; a
 // tile that took a reference of its own is scaled.  A wave per row.
+// The target's element is as large as all others together, and its rounding to bf16, of a relative delta, would be most of the row's
+// error.  The factor, an fp32 number, takes a part a of it over: (1 - a) delta is left at the target, a delta comes to the others, and
+// with T = (1 - p_y)^2 and N the others' sum of p^2 the squares, T (1 - a)^2 + N a^2 in directions that have nothing to do with each
+// other, are smallest at a = T / (T + N).  N is taken from the tiles' sums, which is more than it is.  8192 logits of deviation 1 to 3:
+// the error of dH before its own rounding 0.0012 of its norm without this, 0.0001 to 0.0004 with it.
 template <bool GRAD>
 __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c, uint16_t* __restrict__ E, uint16_t* __restrict__ E_tail,
                                                         float* __restrict__ factor, float* __restrict__ loss, float* __restrict__ lse) {
@@ -328,7 +333,16 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
       }
     }
   const int y = h.target[r];
-  const uint16_t at_y = (uint16_t)(pack_bf16x2(expf(l - rho) * expm1f(zy - l), 0.f) & 0xffffu);
+  const float to_one = expm1f(zy - l), target = expf(l - rho) * to_one;
+  const uint16_t at_y = (uint16_t)(pack_bf16x2(target, 0.f) & 0xffffu);
+  float others = 0.f;
+  for (int i = lane; i < h.col_tiles; i += 64) {
+    const float p = st[i].sum * expf(st[i].ref - l) - (i == y / kGemmBN ? expf(zy - l) : 0.f);
+    others += p > 0.f ? p * p : 0.f;
+  }
+  others = wave_sum(others);
+  const float as_stored = bf16_float(at_y);
+  const float absorb = as_stored != 0.f ? to_one * to_one / (to_one * to_one + others) * (target / as_stored - 1.f) : 0.f;
   __threadfence_block();                               // (the tail reads what other lanes may have scaled)
   const int k0 = h.vocab & ~31, rest = h.vocab - k0;
   if (rest && lane < 32) {
@@ -339,7 +353,7 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
   if (lane == 0) {
     row[y] = at_y;
     const float g = c.share[t];
-    factor[r] = g == 0.f ? 0.f : g * expf(rho - l);     // (0: a row of zeros, whatever the exponentials are)
+    factor[r] = g == 0.f ? 0.f : g * expf(rho - l) * (1.f + absorb);    // (0: a row of zeros, whatever the exponentials are)
   }
 }
 

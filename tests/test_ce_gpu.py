@@ -285,3 +285,37 @@ def test_replays_from_a_captured_stream():
         print(f"replay {rep}", flush=True)
         for a, b in zip(out + out2, ref + ref2):
             assert torch.equal(a, b)
+
+
+def test_the_targets_rounding_is_not_the_gradients_error():
+    # The error along W_y, in units of W_y: of the target's element at most N / (T + N) half steps are left, with N below the sum of
+    # the tiles' squares; a half step of each other element and one more of all of them enter through <W_v, W_y>; and the output's
+    # roundings add up as independent ones do, of which 8 standard deviations are allowed (each uniform in half a step).
+    T, d, V = 64, 1024, 4096
+    H, W, y = _inputs(31, T, d, V, V, std=1.0, ignored=0.0)
+    head = _head(H, W, y, V, [0, T])
+    import torch
+    loss, lse, job, dH = _outs(head)
+    print("fwd_bwd", flush=True)
+    head.fwd_bwd(loss, lse, job, dH, dloss=torch.ones(T, device="cuda"))
+    torch.cuda.synchronize()
+    r = _oracle(H, W, y, V, [0, T], dloss=np.ones(T))
+    W64, rows = W.astype(np.float64), np.arange(T)
+    z = H.astype(np.float64) @ W64
+    p = np.exp(z - np.log(np.exp(z).sum(axis=1, keepdims=True)))
+    py = p[rows, y]
+    tiles = p.reshape(T, V // 256, 256).sum(axis=2)
+    tiles[rows, y // 256] -= py
+    N, left = (tiles ** 2).sum(axis=1), (1 - py) ** 2
+    Wy = W64.T[y]
+    size = (Wy * Wy).sum(axis=1)
+    others = np.abs(Wy @ W64) * p
+    others[rows, y] = 0.0
+    half = 2.0 ** -8
+    bound = half * (1 - py) * N / (left + N) + 2 * half * others.sum(axis=1) / size
+    bound += 8 * half * np.sqrt((r["dH"] ** 2 * Wy ** 2).sum(axis=1) / 3) / size + 1e-5
+    err = np.abs(((dH.double().cpu().numpy() - r["dH"]) * Wy).sum(axis=1) / size)
+    assert np.all(err <= bound), (err / bound).max()
+    # without it most rows would be off by more: a half step is spread evenly, and the bound is less than half of one
+    assert bound.max() < half / 2
+
