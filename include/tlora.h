@@ -380,7 +380,7 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  * dloss NULL, of L = sum_j job_loss_j.  W is frozen: no gradient.
  * Pieces of at most 4096 tokens are taken one after the other, and of a piece the exponentials exp(z) are kept as bf16 between the two
  * products (half a step of a bf16 number off, as the probabilities of tlora_attention_*; the rounding of softmax - 1 at the target,
- * the largest term, is mostly made good by the row's factor, which moves the others by half a step at most); logits are never stored.  Logits, sums and
+ * the largest term, is mostly made good by the row's factor, which moves the others by half a step at most); logits are not kept.  Logits, sums and
  * statistics are fp32.  loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
  * bf16 only (TLORA_EDTYPE otherwise); d_model a multiple of 8; vocab >= 1, of any size; ld_w a multiple of 8, vocab <= ld_w <=
  * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned; outputs overlap no inputs.

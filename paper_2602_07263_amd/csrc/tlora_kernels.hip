@@ -1107,7 +1107,8 @@ __global__ void __launch_bounds__(512) seg_gemm_kernel(GemmParams P) {
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // HEAD: the two waves of a SIMD have different halves of the rows, so that a tile without rows in its second half takes half the time
+  // HEAD: the two waves of a SIMD have different halves of the rows, so that a tile without rows in its second half has half the
+  // products on every SIMD
   const int wm = HEAD ? wave >> 2 : wave & 1, wn = HEAD ? wave & 3 : wave >> 1;
 
   // Workgroup ids are dealt round-robin to the 8 XCDs; hand each XCD a contiguous run of logical tile
