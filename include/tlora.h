@@ -374,8 +374,8 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  *     job_loss_j = sum_{t of job j} w_t loss_t / sum_{t of job j} w_t
  * targets (DEVICE int32 [T]) outside [0, vocab) mark tokens without a loss (prompts, padding): their loss, lse and dH rows are
  * zero, whatever their H row holds, and they enter no sum.  weights (DEVICE fp32 [T], finite; NULL = ones); a
- * token of weight 0 has a loss, but neither that nor its H row enters a mean or a gradient (dH row zero).  A job whose
- * weights sum to zero has job_loss 0 and no gradient.
+ * token of weight 0 has a loss, but neither that nor its H row enters a mean or a gradient (dH row zero, with dloss too).  A job whose
+ * weights sum to zero has job_loss 0, of which there is no gradient.  Other weights than 0 have no say in a gradient made from dloss.
  * tlora_ce_fwd_bwd also makes  dH_t = g_t (softmax(z_t) - onehot(y_t)) . W^T  with g_t = dloss[t] (DEVICE fp32 [T]) or, with
  * dloss NULL, of L = sum_j job_loss_j.  W is frozen: no gradient.
  * Pieces of at most 4096 tokens are taken one after the other, and of a piece the exponentials exp(z) are kept as bf16 between the two

@@ -35,8 +35,8 @@ __device__ __forceinline__ double block_sum_1024(double x, double* red) {
 
 // ---------------------------------------------------------------------------------------------------
 // Cross entropy.  Workgroup 0 lists the tokens that have a loss, in token order; workgroup 1 + j sums job j's weights and notes
-// what each of its tokens' losses counts for (dloss, or weight / sum).  Tokens without a loss get zeros.  Of the workgroups behind
-// those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the batch is one
+// what each of its tokens' losses counts for (dloss, or weight / sum; nothing at weight 0).  Tokens without a loss get zeros.  Of the
+// workgroups behind those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the batch is one
 // piece moves the others' rows of H to their places, for which it counts the list up to its tokens itself (16 KB of targets at
 // most, from the L2; a launch of its own that reads the list would cost more); the last copy the end of W.
 // ---------------------------------------------------------------------------------------------------
@@ -114,8 +114,10 @@ __global__ void __launch_bounds__(1024) ce_prepare_kernel(CeTokens c, int num_jo
     for (int t = a + tid; t < b; t += 1024) {
       float g = 0.f;
       if (ce_live(c.targets[t], c.vocab)) {
-        if (p.dloss) g = p.dloss[t];
-        else if (total != 0.0) g = (float)((c.weights ? (double)c.weights[t] : 1.0) / total);
+        const double v = c.weights ? (double)c.weights[t] : 1.0;
+        if (v == 0.0) g = 0.f;                         // (a token of weight 0 is left out, whatever the caller's gradient is)
+        else if (p.dloss) g = p.dloss[t];
+        else if (total != 0.0) g = (float)(v / total);
       }
       c.share[t] = g;
     }
