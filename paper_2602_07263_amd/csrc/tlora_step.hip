@@ -273,8 +273,9 @@ __global__ void __launch_bounds__(256) head_grad_reduce_kernel(const float* __re
 
 // A row's statistics become its logarithm of the sum and its loss; with GRAD its exponentials become those of the gradient: all
 // relative to one reference rho, the target's less the sum itself, and factor = share * exp(rho - lse).  rho is 0 unless the sum
-// itself is out of range for it, so that as a rule (logits within head_reference's bounds) one element of the row is touched; a
-// tile that took a reference of its own is scaled.  A wave per row.
+// itself is out of range for it or the factor would be (a gradient from above of 1e-20 beside lse 57 left a subnormal factor and a row
+// wrong by a third), so that as a rule (logits within head_reference's bounds) one element of the row is touched; a tile that took a
+// reference of its own is scaled.  A wave per row.
 // The target's element is as large as all others together, and its rounding to bf16, of a relative delta, would be most of the row's
 // error.  The factor, an fp32 number, takes a part a of it over: (1 - a) delta is left at the target, a delta comes to the others, and
 // with T = (1 - p_y)^2 and N the others' sum of p^2 the squares, T (1 - a)^2 + N a^2 in directions that have nothing to do with each
@@ -315,7 +316,9 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
     if (lse) lse[t] = l;
   }
   if (!GRAD) return;
-  const float rho = l >= -20.f && l <= 60.f ? 0.f : l;     // (share * exp(-60) is still an ordinary number)
+  // (one row has one share: all lanes agree.  With rho = l the factor is the share itself)
+  const float g = c.share[t], at_zero = fabsf(g) * expf(-l);
+  const float rho = l >= -20.f && l <= 60.f && (g == 0.f || (at_zero >= 0x1p-100f && at_zero <= 0x1p100f)) ? 0.f : l;
   uint16_t* const row = E + (int64_t)r * h.ld;
   const int n8 = (h.vocab + 7) & ~7;
   if (!plain || rho != 0.f)
@@ -354,7 +357,6 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
   }
   if (lane == 0) {
     row[y] = at_y;
-    const float g = c.share[t];
     factor[r] = g == 0.f ? 0.f : g * expf(rho - l) * (1.f + absorb);    // (0: a row of zeros, whatever the exponentials are)
   }
 }
