@@ -347,8 +347,8 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
  * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs
  * gamma_post (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or added to with TLORA_BWD_ACCUMULATE (the only flag);
  * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap no inputs.
- * mean(V^2) + eps of a row is to lie between 2^-80 and 2^80: its powers are fp32 numbers, and outside (a row of zeros with eps 0, say)
- * that row, and the sums it enters, may be infinite or not a number.
+ * mean(V^2) + eps of a row is to lie between 2^-80 and 2^80, and results and their terms are to be ordinary fp32 numbers; outside (a row of
+ * zeros with eps 0, say) that row, and the sums it enters, may be infinite, not a number or wrong.
  * tlora_norm_fwd needs no workspace.  tlora_norm_bwd's: 256-byte aligned, tlora_norm_workspace_bytes.  Neither call allocates,
  * copies or synchronises, so both may be captured into a graph. */
 typedef struct {

@@ -597,11 +597,20 @@ __device__ __forceinline__ float rstd_of(float x) {
   return x > 0.f && x < __builtin_huge_valf() ? better : r;
 }
 
+// D = dH + r2 (u - c2 hn) with u = dXn gamma_pre, hn = r2 H and c2 = mean(u hn); dY = r1 (v - c1 (r1 Y)) with v = res_scale gate
+// gamma_post D and c1 = mean(v r1 Y).  Every reciprocal root stands beside the value that it is of: its square or cube would leave
+// fp32 where the result does not.  Fused operations written out, so that every kernel rounds alike.
+__device__ __forceinline__ float norm_D(float dH, float u, float hn, float r2, float c2) { return fmaf(r2, fmaf(-hn, c2, u), dH); }
+__device__ __forceinline__ float norm_dY(float v, float y, float r1, float c1) { return r1 * fmaf(-(y * r1), c1, v); }
+// sum D w, from the sums of dH w, u w and H w
+__device__ __forceinline__ float norm_dot(float dHw, float uw, float hw, float r2, float c2) {
+  return fmaf(r2, fmaf(-c2, r2 * hw, uw), dHw);
+}
+
 // Backward of a unit's rows, one after the other; with SUMS the unit's column sums stay in registers and leave as partial
 // [unit][3][d] (dgamma_post, dgamma_pre, dgate; those that are wanted).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
 // for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
-// what the second sums give, D = dH + r2 (dXn gamma_pre) - k2 H, so the last sum is put together from three that need rstd_Y
-// alone; and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
+// what the second sums give (norm_D), so the last sum is put together from three that need rstd_Y alone (norm_dot); and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
 // barrier.  31744 x 4096 bf16 with all sums 320 us (4.9 TB/s).
 // BOTH: dX and dY are wanted.  Every lane then stores without a condition -- those behind the row's end its last features once more,
 // the same values -- since behind a store that may not have been issued the compiler waits for all those that may.
@@ -678,24 +687,25 @@ __global__ void __launch_bounds__(norm_bwd_row(BF) / 8) norm_bwd_unit_kernel(Nor
 #pragma unroll
     for (int i = 0; i < 5; ++i) s[i] = on ? s[i] : 0.f;
     norm_sums(s, red[(t - t0) & 1]);
-    float r2 = 0.f, k2 = 0.f;
+    float r2 = 0.f, c2 = 0.f;
     if (g.dXn) {
       r2 = rstd_of(s[0] * inv_d + a.eps);
-      k2 = s[1] * r2 * r2 * r2 * inv_d;
+      c2 = s[1] * r2 * inv_d;
     }
-    const float k1 = a.gamma_post ? (s[2] + r2 * s[3] - k2 * s[4]) * r1 * r1 * r1 * inv_d : 0.f;
+    const float c1 = a.gamma_post ? norm_dot(s[2], s[3], s[4], r2, c2) * r1 * inv_d : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      D[e] += r2 * (gq[e] * q[e]) - h[e] * k2;
+      const float hn = h[e] * r2;
+      D[e] = norm_D(D[e], gq[e] * q[e], hn, r2, c2);
       if (SUMS) {
         sum_y[e] += D[e] * (y[e] * r1);
-        sum_h[e] += gq[e] * (h[e] * r2);
+        sum_h[e] += gq[e] * hn;
       }
     }
     if (BOTH || g.dX) store8<BF>(g.dX, at, D);
     if (BOTH || g.dY) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) D[e] = r1 * (agp[e] * D[e]) - y[e] * k1;
+      for (int e = 0; e < 8; ++e) D[e] = norm_dY(agp[e] * D[e], y[e], r1, c1);
       store8<BF>(g.dY, at, D);
     }
 #pragma unroll
@@ -717,9 +727,9 @@ __global__ void __launch_bounds__(norm_bwd_row(BF) / 8) norm_bwd_unit_kernel(Nor
   }
 }
 
-// rstd of Y and of H, and the factor of H in D = dH + r2 (dXn gamma_pre) - H k2
+// rstd of Y and of H, and c2 of norm_D
 struct NormRow {
-  float r1, r2, k2, pad;
+  float r1, r2, c2, pad;
 };
 
 // Backward of one row per workgroup, two runs per thread; the column sums are left to norm_bwd_cols_kernel.
@@ -775,26 +785,26 @@ __global__ void __launch_bounds__(1024) norm_bwd_row_kernel(NormArgs a, NormJobs
     }
   }
   norm_sums(s, red[1]);
-  float r2 = 0.f, k2 = 0.f;
+  float r2 = 0.f, c2 = 0.f;
   if (g.dXn) {
     r2 = rstd_of(s[0] * inv_d + a.eps);
-    k2 = s[1] * r2 * r2 * r2 * inv_d;
+    c2 = s[1] * r2 * inv_d;
   }
-  const float k1 = a.gamma_post ? (s[2] + r2 * s[3] - k2 * s[4]) * r1 * r1 * r1 * inv_d : 0.f;
-  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, k2, 0.f};
+  const float c1 = a.gamma_post ? norm_dot(s[2], s[3], s[4], r2, c2) * r1 * inv_d : 0.f;
+  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, c2, 0.f};
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int c = c0 + k * step;
     if (c >= a.d) continue;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) D[k][e] += r2 * gq[k][e] - h[k][e] * k2;
+    for (int e = 0; e < 8; ++e) D[k][e] = norm_D(D[k][e], gq[k][e], h[k][e] * r2, r2, c2);
     if (g.dX) store8<BF>(g.dX, row + c, D[k]);
     if (g.dY) {
       float agp[8], p[8];
       load8_or<BF>(jb.gate, c, 1.f, agp);
       load8_or<BF>(a.gamma_post, c, 1.f, p);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) D[k][e] = r1 * (agp[e] * (p[e] * a.res_scale) * D[k][e]) - y[k][e] * k1;
+      for (int e = 0; e < 8; ++e) D[k][e] = norm_dY(agp[e] * (p[e] * a.res_scale) * D[k][e], y[k][e], r1, c1);
       store8<BF>(g.dY, row + c, D[k]);
     }
   }
@@ -803,7 +813,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_row_kernel(NormArgs a, NormJobs
 // ---- wider rows: read again for every sum -----------------------------------------------------------------------------------
 template <bool BF>
 __device__ __forceinline__ void norm_elements(const NormArgs& a, const void* gate, const NormGrads& g, int64_t row, int c, float r1, float r2,
-                                              float k2, float (&y)[8], float (&pn)[8], float (&h)[8], float (&gn)[8], float (&D)[8],
+                                              float c2, float (&y)[8], float (&pn)[8], float (&h)[8], float (&gn)[8], float (&D)[8],
                                               float (&ag)[8]) {
   float p[8];
   load8<BF>(a.Y, row + c, y);
@@ -819,7 +829,7 @@ __device__ __forceinline__ void norm_elements(const NormArgs& a, const void* gat
     pn[e] = p[e];
     ag[e] *= a.res_scale;
     h[e] += ag[e] * (y[e] * r1 * p[e]);
-    D[e] += r2 * (gn[e] * q[e]) - h[e] * k2;
+    D[e] = norm_D(D[e], gn[e] * q[e], h[e] * r2, r2, c2);
   }
 }
 
@@ -831,7 +841,7 @@ __global__ void __launch_bounds__(256) norm_bwd_rows_kernel(NormArgs a, NormJobs
   const int t = jb.row0 + (int)blockIdx.x - jb.unit0;
   const int64_t row = (int64_t)t * a.d;
   const float inv_d = 1.0f / (float)a.d;
-  float r1 = 1.f, r2 = 0.f, k2 = 0.f;
+  float r1 = 1.f, r2 = 0.f, c2 = 0.f;
   if (a.gamma_post) {
     float ss = 0.f;
     for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
@@ -856,26 +866,26 @@ __global__ void __launch_bounds__(256) norm_bwd_rows_kernel(NormArgs a, NormJobs
       }
     }
     r2 = 1.0f / sqrtf(block_sum(ss, red) * inv_d + a.eps);
-    k2 = block_sum(dot, red) * r2 * r2 * r2 * inv_d;
+    c2 = block_sum(dot, red) * r2 * inv_d;
   }
-  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, k2, 0.f};
-  float k1 = 0.f;
+  if (rows && threadIdx.x == 0) rows[t] = NormRow{r1, r2, c2, 0.f};
+  float c1 = 0.f;
   if (a.gamma_post && g.dY) {
     float dot = 0.f;
     for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
-      norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, k2, y, p, h, gn, D, ag);
+      norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, c2, y, p, h, gn, D, ag);
 #pragma unroll
       for (int e = 0; e < 8; ++e) dot += ag[e] * D[e] * p[e] * y[e];
     }
-    k1 = block_sum(dot, red) * r1 * r1 * r1 * inv_d;
+    c1 = block_sum(dot, red) * r1 * inv_d;
   }
   if (!g.dX && !g.dY) return;
   for (int c = threadIdx.x * 8; c < a.d; c += 2048) {
-    norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, k2, y, p, h, gn, D, ag);
+    norm_elements<BF>(a, jb.gate, g, row, c, r1, r2, c2, y, p, h, gn, D, ag);
     if (g.dX) store8<BF>(g.dX, row + c, D);
     if (g.dY) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) D[e] = r1 * (ag[e] * D[e] * p[e]) - y[e] * k1;
+      for (int e = 0; e < 8; ++e) D[e] = norm_dY(ag[e] * D[e] * p[e], y[e], r1, c1);
       store8<BF>(g.dY, row + c, D);
     }
   }
@@ -895,7 +905,7 @@ __global__ void __launch_bounds__(256) norm_bwd_cols_kernel(NormArgs a, NormJobs
     for (int t = t0 + wave; t < t1; t += 4) {
       const NormRow r = rows[t];
       float y[8], p[8], h[8], gn[8], D[8], ag[8];
-      norm_elements<BF>(a, jb.gate, g, (int64_t)t * a.d, c, r.r1, r.r2, r.k2, y, p, h, gn, D, ag);
+      norm_elements<BF>(a, jb.gate, g, (int64_t)t * a.d, c, r.r1, r.r2, r.c2, y, p, h, gn, D, ag);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float yn = y[e] * r.r1;

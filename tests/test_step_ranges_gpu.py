@@ -3,7 +3,9 @@ and test_norm_gpu."""
 import numpy as np
 import pytest
 
+from oracle import norm_oracle as no
 from tests import test_ce_gpu as tc
+from tests import test_norm_gpu as tn
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +65,43 @@ def test_upstream_gradients_far_from_one(shift, size):
     err = size_of(out[3].double().cpu().numpy()[at, :-1] - want)
     assert np.all(err <= 1.01 * bound), (err / bound).max()
     assert np.all(bound <= 0.2 * size_of(want))
+
+
+# Mean squares of 2^80 and 2^-80, with gradients from above whose products with powers of 1 / rms leave fp32 where two or three of them
+# come together, although each result is an ordinary number.  Widths of every variant of the backward.
+WIDTHS = [("bf16", 256), ("f32", 1544), ("bf16", 8200), ("f32", 4104), ("bf16", 17408)]
+
+
+@pytest.mark.parametrize("alone,size,upstream", [(True, 40, -60), (True, -40, 60), (False, 40, -50), (False, -40, 20)])
+@pytest.mark.parametrize("dtype,d", WIDTHS, ids=[f"{t}_{d}" for t, d in WIDTHS])
+def test_norm_of_rows_far_from_unit_size(dtype, d, alone, size, upstream):
+    import torch
+    from paper_2602_07263_amd import tlora
+    T, off, half = 9, [0, 5, 9], 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    v = tn._draw(61 + d, dtype, T, d, 2, post=not alone, gates=not alone, X=not alone)
+    for k in ("X", "Y"):
+        v[k] = None if v[k] is None else np.ldexp(v[k], size)
+    for k in ("dH", "dXn"):
+        v[k] = np.ldexp(v[k], upstream)
+    if alone:
+        v["dH"] = None
+    kw = dict(gamma_post=v["gamma_post"], gamma_pre=v["gamma_pre"], gates=v["gates"])
+    r = no.backward(v["X"], v["Y"], off, 0.0, v["dH"], v["dXn"], 0.5, **kw)
+    up = lambda a: tn._up(a, dtype)
+    n = tlora.ResidualNorm(dtype, off, up(v["X"]), up(v["Y"]), up(v["gamma_pre"]), 0.0, gamma_post=up(v["gamma_post"]),
+                           gates=None if alone else [up(g) for g in v["gates"]], res_scale=0.5)
+    Y = n._keep[1]
+    dX, dY = tn._nan_like(Y), tn._nan_like(Y)
+    sums = [tn._nan_like(Y, d, True) for _ in range(4)]
+    print(f"bwd {dtype} {d} {alone} {size}", flush=True)
+    n.bwd(up(v["dH"]), up(v["dXn"]), dX, dY, dgamma_pre=sums[0], dgamma_post=None if alone else sums[1],
+          dgates=None if alone else sums[2:])
+    torch.cuda.synchronize()
+    tn._near(dX, r["dX"], r["abs_dX"], half, "dX")
+    tn._near(dY, r["dY"], r["abs_dY"], half, "dY")
+    chain = 1 + (T / 512 + 64) / 64
+    tn._near(sums[0], r["dgamma_pre"], chain * r["abs_dgamma_pre"], 2.0 ** -24, "dgamma_pre")
+    if not alone:
+        tn._near(sums[1], r["dgamma_post"], chain * r["abs_dgamma_post"], 2.0 ** -24, "dgamma_post")
+        for j in range(2):
+            tn._near(sums[2 + j], r["dgates"][j], chain * r["abs_dgates"][j], 2.0 ** -24, f"dgate {j}")
