@@ -413,8 +413,11 @@ int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float
  * groups in all (TLORA_EINVAL otherwise); X: DEVICE [T, d] of `dtype`, 16-byte aligned.
  * tlora_bwd_ckpt is tlora_bwd of the problem whose X are the packed values x^: p->X is not read and may be NULL.  With
  * TLORA_BWD_REUSE_S the S_j of the tlora_fwd before it on this workspace are taken (made from the X that the forward had), otherwise
- * S_j = X^_j.A_j.  Its workspace, tlora_ckpt_workspace_bytes, begins with that of tlora_fwd / tlora_bwd of the problem; flags and
- * everything else as tlora_bwd. */
+ * S_j = X^_j.A_j.  Its workspace begins with that of tlora_fwd / tlora_bwd of the problem.  That alone (tlora_workspace_bytes) is
+ * enough for calls without dA / dB and, of bf16 values with d_in a multiple of 16, for calls with TLORA_BWD_REUSE_S, whose
+ * workspace lives from the forward to the backward; behind it calls that need the values themselves have room for them.
+ * tlora_ckpt_workspace_bytes is enough for every call on the problem, or on one of the same dtype, d_in, d_out, J and ranks in which no job has
+ * more tokens.  Flags and everything else as tlora_bwd. */
 #define TLORA_CKPT_GROUP 128
 size_t tlora_ckpt_bytes(int64_t tokens, int32_t d);
 int tlora_ckpt_pack(int32_t dtype, const void* X, int64_t tokens, int32_t d, void* packed, void* hip_stream);

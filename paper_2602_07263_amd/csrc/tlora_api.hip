@@ -279,6 +279,7 @@ void build_grad_units(const Plan& pl, int D, double limit, bool idle_units, std:
 // workgroup slots (80 KB of LDS each, two per CU), while a split keeps at least 4 K-steps of 64 (three are in flight
 // before the first is multiplied).  Fewer if the fp32 sums (4 bytes per packed S element and split) would not fit.
 constexpr int kGemmMaxSplits = 16;
+constexpr int kWideUnits = 192;                          // units of a streaming shrink from which on they have more than 32 rows
 constexpr int kShrinkSlots = 512, kShrinkMinSteps = 4, kShrinkMaxSplits = 32;
 int shrink_splits(const Plan& pl, int K, size_t max_bytes) {
   if (pl.shrink_rows != 32 || g_opt.shrink_rows != 0 || K % 64 || pl.stream_units.empty()) return 1;
@@ -519,7 +520,7 @@ int build_plan(const tlora_problem_t* p, Plan& pl, bool fwd_only = false) {
       if (generic > kMaxUnits || count(32) > kMaxUnits) return TLORA_EINVAL;
       const bool can32 = pl.d_in % 64 == 0 && pl.d_out % 64 == 0;
       if (g_opt.shrink_rows != 0) pl.shrink_rows = (g_opt.shrink_rows == 32 && !can32) ? 64 : g_opt.shrink_rows;
-      else pl.shrink_rows = count(128) >= 192 ? 128 : (count(64) >= 192 || !can32) ? 64 : 32;
+      else pl.shrink_rows = count(128) >= kWideUnits ? 128 : (count(64) >= kWideUnits || !can32) ? 64 : 32;
     }
     for (int j = 0; j < pl.J; ++j) {
       const JobDev& jb = pl.jobs[j];
@@ -2465,11 +2466,33 @@ int tlora_ckpt_unpack(int32_t dtype, const void* packed, int64_t tokens, int32_t
   return launches_ok(__LINE__);
 }
 
+namespace {
+// Whether tlora_bwd_ckpt unpacks X.  X enters the adapters' gradients alone: dA_j, and S_j where it is to be made again.  The codes serve
+// both as they are where rows are whole 16-byte pieces and the shrink is a streaming one; a small batch's forms of it take the values.
+bool ckpt_unpacks(const Plan& pl, int flags, bool grads) {
+  if (!grads) return false;
+  return pl.dtype != TLORA_BF16 || pl.d_in % 16 || (!(flags & TLORA_BWD_REUSE_S) && !shrink_takes_codes(pl));
+}
+size_t ckpt_bytes_behind(const Plan& pl, int64_t tokens) {
+  const size_t elt = pl.dtype == TLORA_F32 ? 4 : 2;
+  return align_up(align_up(pl.total, 256) + elt * (size_t)tokens * (size_t)pl.d_in, 256);
+}
+// Tokens of the largest batch that calls of any flags may unpack and in which no job has more tokens than here: all, or, where large
+// batches are taken from the codes, those of a plan with fewer than kWideUnits units of 64 rows.  (Jobs of rank 0 have no units.)
+int64_t ckpt_most_unpacked(const Plan& pl) {
+  const int groups = (pl.d_in + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
+  if (pl.dtype != TLORA_BF16 || pl.d_in % 64 || g_opt.shrink_rows != 0 || groups * 128 > kShrinkScales) return pl.T;
+  int64_t ranked = 0;
+  for (const JobDev& jb : pl.jobs) ranked += jb.rpad > 0 ? jb.row1 - jb.row0 : 0;
+  return pl.T - ranked + std::min<int64_t>(ranked, 64 * kWideUnits);
+}
+}  // namespace
+
 size_t tlora_ckpt_workspace_bytes(const tlora_problem_t* p) {
-  const size_t inner = tlora_workspace_bytes(p);
-  if (inner == 0 || ckpt_sizes(p->offsets[p->num_jobs], p->d_in) != TLORA_OK) return 0;
-  const size_t elt = p->dtype == TLORA_F32 ? 4 : 2;
-  return align_up(align_up(inner, 256) + elt * (size_t)p->offsets[p->num_jobs] * (size_t)p->d_in, 256);
+  std::lock_guard<std::recursive_mutex> lk(g_mu);
+  const PlanEntry* e = nullptr;
+  if (get_plan(p, false, &e) != TLORA_OK || ckpt_sizes(e->pl.T, e->pl.d_in) != TLORA_OK) return 0;
+  return ckpt_bytes_behind(e->pl, ckpt_most_unpacked(e->pl));
 }
 
 int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY, void* dX, void* const* dA, void* const* dB,
@@ -2480,17 +2503,20 @@ int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY,
   const int64_t T = p->offsets[p->num_jobs];
   rc = ckpt_sizes(T, p->d_in);
   if (rc != TLORA_OK) return rc;
-  const size_t need = tlora_ckpt_workspace_bytes(p), inner = align_up(tlora_workspace_bytes(p), 256);
-  if (bad_ws(workspace, ws_bytes, need)) return TLORA_EWORKSPACE;
+  const PlanEntry* entry = nullptr;
+  rc = get_plan(p, false, &entry);
+  if (rc != TLORA_OK) return rc;
+  const bool unpacks = ckpt_unpacks(entry->pl, flags, dA != nullptr);
+  const size_t inner = align_up(entry->pl.total, 256);
+  if (bad_ws(workspace, ws_bytes, unpacks ? ckpt_bytes_behind(entry->pl, T) : entry->pl.total)) return TLORA_EWORKSPACE;
   if (T > 0 && !packed) return TLORA_ENULL;
   if (reinterpret_cast<uintptr_t>(packed) & 255) return TLORA_EALIGN;
   tlora_problem_t q = *p;
-  uint8_t* const X = static_cast<uint8_t*>(workspace) + inner;
+  uint8_t* const X = static_cast<uint8_t*>(workspace) + (unpacks ? inner : 0);     // (an address for what is not read either)
   q.X = X;
   // (everything is checked before the first launch)
-  const PlanEntry* entry = nullptr;
   std::vector<JobDev> hjobs;
-  rc = common_checks(&q, &entry, hjobs, workspace, inner);
+  rc = common_checks(&q, &entry, hjobs, workspace, ws_bytes);
   if (rc != TLORA_OK) return rc;
   if (T > 0 && !dY) return TLORA_ENULL;
   if ((dA == nullptr) != (dB == nullptr)) return TLORA_ENULL;
@@ -2499,18 +2525,16 @@ int tlora_bwd_ckpt(const tlora_problem_t* p, const void* packed, const void* dY,
     for (int j = 0; j < p->num_jobs; ++j)
       if (p->ranks[j] > 0 && (!dA[j] || !dB[j])) return TLORA_ENULL;
   if (flags & ~(TLORA_BWD_REUSE_S | TLORA_BWD_REUSE_WT | TLORA_BWD_ACCUMULATE)) return TLORA_EINVAL;
-  // X enters the adapters' gradients alone: dA_j, and S_j where it is to be made again.  The codes serve both as they are where rows are
-  // whole 16-byte pieces and the shrink is a streaming one; a small batch's forms of it take the values.
   PackedX x;
-  if (dA && p->dtype == TLORA_BF16 && p->d_in % 16 == 0 && ((flags & TLORA_BWD_REUSE_S) || shrink_takes_codes(entry->pl))) {
+  if (dA && !unpacks) {
     x.codes = static_cast<const uint8_t*>(packed);
     x.scales = reinterpret_cast<const uint16_t*>(x.codes + ckpt_scales_at(T, p->d_in));
     x.groups = (p->d_in + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
-  } else if (dA) {
+  } else if (unpacks) {
     rc = tlora_ckpt_unpack(p->dtype, packed, T, p->d_in, X, hip_stream);
     if (rc != TLORA_OK) return rc;
   }
-  return bwd_impl(&q, dY, dX, dA, dB, flags, workspace, inner, hip_stream, nullptr, nullptr, nullptr, nullptr, nullptr, 0, x);
+  return bwd_impl(&q, dY, dX, dA, dB, flags, workspace, ws_bytes, hip_stream, nullptr, nullptr, nullptr, nullptr, nullptr, 0, x);
 }
 
 // ---- general token -> adapter assignment (Sec. 3.3: tokens of an adapter are gathered, results scattered back) ----

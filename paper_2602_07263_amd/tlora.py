@@ -549,11 +549,14 @@ class LayerProblem:
                   None if dB is None else [b.data_ptr() if b.numel() else 0 for b in dB],
                   (TLORA_BWD_REUSE_S if reuse_S else 0) | flags, self.ws.data_ptr(), self.ws_bytes, self._stream())
 
-    def bwd_ckpt_workspace(self) -> None:
-        """Grow the workspace to what bwd_ckpt needs.  Before the fwd whose S_j bwd_ckpt is to reuse: a new one is empty."""
+    def bwd_ckpt_workspace(self, reuse_S: bool = False) -> None:
+        """Grow the workspace to what bwd_ckpt needs.  Before the fwd whose S_j bwd_ckpt is to reuse: a new one is empty.
+        reuse_S: for calls with reuse_S alone, which of bf16 values with d_in a multiple of 16 need no more than fwd and bwd."""
         need = int(lib().tlora_ckpt_workspace_bytes(ctypes.byref(self.prob)))
         if need == 0:
             raise TloraError("tlora_ckpt_workspace_bytes: invalid problem")
+        if reuse_S and self.dtype == "bf16" and self.d_in % 16 == 0:
+            return
         if need > self.ws_bytes:
             self.ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.X.device)
             self.ws_bytes = need

@@ -1,0 +1,71 @@
+"""Workspaces of the operators around the decoder layers: what they hold beside the plain ones, on the host."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2602_07263_amd import tlora
+
+P = ctypes.c_void_p
+WS = 0x100000
+EWORKSPACE, ENOUGH = -4, -7
+
+
+def _problem(tokens, ranks, d_in, d_out=4096, dtype=tlora.TLORA_BF16):
+    off = np.concatenate([[0], np.cumsum(tokens)]).astype(np.int64)
+    n = len(ranks)
+    return tlora.make_problem(dtype, d_in, d_out, ranks, off, [1.0] * n, 0, 0x2000, [0x3000] * n, [0x4000] * n)
+
+
+def _sizes(q):
+    L = tlora.lib()
+    return L.tlora_workspace_bytes(ctypes.byref(q[0])), L.tlora_ckpt_workspace_bytes(ctypes.byref(q[0]))
+
+
+def _rc(q, n, flags=0, grads=True):
+    """EWORKSPACE, or what a call whose workspace is large enough is refused for next: packed values that are not aligned."""
+    g = (P * q[0].num_jobs)(*[0x6000] * q[0].num_jobs) if grads else None
+    return tlora.lib().tlora_bwd_ckpt(ctypes.byref(q[0]), P(WS + 16), P(0x5000), P(0x8000), g, g, flags, P(WS), n, None)
+
+
+BATCH_8B = ([5120, 512, 2048, 3584, 3072, 6144, 5120, 6144], [4, 8, 8, 16, 32, 32, 64, 128])
+
+
+def test_a_kept_S_needs_no_room_for_the_values():
+    for d_in in (4096, 12288, 17408, 144):
+        q = _problem(*BATCH_8B, d_in)
+        plain, with_values = _sizes(q)
+        assert _rc(q, plain - 1, tlora.TLORA_BWD_REUSE_S) == EWORKSPACE
+        assert _rc(q, plain, tlora.TLORA_BWD_REUSE_S) == ENOUGH
+        assert _rc(q, plain, grads=False) == ENOUGH
+        assert with_values > plain
+
+
+def test_large_batches_have_room_for_what_small_ones_unpack():
+    T = sum(BATCH_8B[0])
+    for d_in in (4096, 12288):
+        plain, with_values = _sizes(_problem(*BATCH_8B, d_in))
+        assert with_values - plain <= 2 * 12288 * d_in + 512 < 2 * T * d_in
+        q = _problem(*BATCH_8B, d_in)
+        assert _rc(q, plain) == ENOUGH              # (S_j is made again from the codes)
+
+
+@pytest.mark.parametrize("kw", [dict(d_in=4096), dict(d_in=4096, d_out=4104), dict(d_in=1000), dict(d_in=144), dict(d_in=24576),
+                                dict(d_in=512, dtype=tlora.TLORA_F32)], ids=lambda k: "_".join(str(v) for v in k.values()))
+@pytest.mark.parametrize("ranks", [[8, 16, 0], [130, 4, 700]])
+def test_a_workspace_serves_every_smaller_batch(kw, ranks):
+    sizes, tokens = [], ([1, 0, 3], [60, 1, 60], [61, 200, 200], [3000, 200, 200], [6000, 3000, 200], [6000, 6000, 6000], [12000, 12000, 6000],
+                         [30000, 12000, 6000], [30000, 40000, 6001])
+    for t in tokens:
+        q = _problem(t, ranks, **kw)
+        plain, most = _sizes(q)
+        # what any call on this batch needs: found by its refusals
+        for flags in (0, tlora.TLORA_BWD_REUSE_S):
+            assert _rc(q, most, flags) == ENOUGH
+        sizes.append(most)
+        values = (4 if kw.get("dtype") == tlora.TLORA_F32 else 2) * sum(t) * kw["d_in"]
+        behind = (plain + 255) // 256 * 256
+        small = _rc(q, plain) == EWORKSPACE
+        if small:                                       # the call unpacks: no byte less than the values take
+            assert _rc(q, behind + values - 1) == EWORKSPACE
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
