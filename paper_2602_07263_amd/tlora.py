@@ -550,16 +550,19 @@ class LayerProblem:
                   (TLORA_BWD_REUSE_S if reuse_S else 0) | flags, self.ws.data_ptr(), self.ws_bytes, self._stream())
 
     def bwd_ckpt_workspace(self, reuse_S: bool = False) -> None:
-        """Grow the workspace to what bwd_ckpt needs.  Before the fwd whose S_j bwd_ckpt is to reuse: a new one is empty.
-        reuse_S: for calls with reuse_S alone, which of bf16 values with d_in a multiple of 16 need no more than fwd and bwd."""
+        """Grow the workspace to what bwd_ckpt needs, with what a fwd has left in it (S_j, the packed adapters).  A graph captured before
+        still has the address of the old one: capture afterwards.  reuse_S: for calls with reuse_S alone, which of bf16 values with d_in a multiple of 16 need no more than fwd and bwd."""
         need = int(lib().tlora_ckpt_workspace_bytes(ctypes.byref(self.prob)))
         if need == 0:
             raise TloraError("tlora_ckpt_workspace_bytes: invalid problem")
         if reuse_S and self.dtype == "bf16" and self.d_in % 16 == 0:
             return
         if need > self.ws_bytes:
-            self.ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.X.device)
-            self.ws_bytes = need
+            grown = self.torch.empty(need, dtype=self.torch.uint8, device=self.X.device)
+            grown[:self.ws_bytes].copy_(self.ws[:self.ws_bytes])
+            if self.ws.is_cuda:                                   # (the copy may run on another stream than the old one came from)
+                self.ws.record_stream(self.torch.cuda.current_stream())
+            self.ws, self.ws_bytes = grown, need
 
     def bwd_ckpt(self, packed, dY, dX, dA, dB, reuse_S: bool = False, flags: int = 0) -> None:
         """bwd from the 8-bit form of X (`packed`: the bytes of Checkpoint.pack); bwd_ckpt_workspace comes first."""

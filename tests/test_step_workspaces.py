@@ -69,3 +69,17 @@ def test_a_workspace_serves_every_smaller_batch(kw, ranks):
         if small:                                       # the call unpacks: no byte less than the values take
             assert _rc(q, behind + values - 1) == EWORKSPACE
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+def test_a_holder_keeps_what_its_workspace_held():
+    import torch
+    bf = torch.bfloat16
+    z = lambda *n: torch.zeros(*n, dtype=bf)
+    layer = tlora.LayerProblem("bf16", 16, 16, [4], [0, 4], [1.0], z(4, 16), z(16, 16), [z(16, 4)], [z(4, 16)])
+    layer.ws.copy_(torch.arange(layer.ws_bytes) % 251)
+    before = layer.ws.clone()
+    layer.bwd_ckpt_workspace(reuse_S=True)
+    assert layer.ws_bytes == before.numel()
+    layer.bwd_ckpt_workspace()
+    assert layer.ws_bytes == layer.ws.numel() > before.numel()
+    assert torch.equal(layer.ws[:before.numel()], before)

@@ -37,3 +37,28 @@ def test_the_plain_workspace_is_enough(d_in, ranks, tokens, reuse_S):
         assert torch.equal(a, b)
     lp.bwd_ckpt_workspace(reuse_S=True)                 # asks for nothing more
     assert lp.ws_bytes == plain
+
+
+def test_a_workspace_that_grows_behind_the_forward_keeps_its_S():
+    import torch
+    from paper_2602_07263_amd import tlora
+    p = wk.generate(wk.custom("ckpt", "f32", 136, 72, [4, 7], [50, 81], [2.0, 1.0]), seed=5)
+    dY, results = torch.from_numpy(p.dY).cuda(), []
+    for late in (False, True):
+        lp = tlora.LayerProblem.from_numpy(p)
+        c = tlora.Checkpoint("f32", lp.T, 136, "cuda")
+        c.pack(lp.X)
+        Y, _, dA, dB = lp.new_outputs()
+        if not late:
+            lp.bwd_ckpt_workspace()
+        lp.fwd(Y)
+        if late:
+            with pytest.raises(tlora.TloraError):       # (a workspace that is too small: refused, nothing is launched)
+                lp.bwd_ckpt(c.packed, dY, None, dA, dB, reuse_S=True)
+            lp.bwd_ckpt_workspace()
+        print(f"late {late}", flush=True)
+        lp.bwd_ckpt(c.packed, dY, None, dA, dB, reuse_S=True)
+        torch.cuda.synchronize()
+        results.append(dA + dB)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
