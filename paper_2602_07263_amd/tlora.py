@@ -566,13 +566,25 @@ class LayerProblem:
 
     def bwd_ckpt(self, packed, dY, dX, dA, dB, reuse_S: bool = False, flags: int = 0) -> None:
         """bwd from the 8-bit form of X (`packed`: the bytes of Checkpoint.pack); bwd_ckpt_workspace comes first."""
+        t, dev = self.torch, self.X.get_device()
         if packed is not None and packed.numel() * packed.element_size() < int(lib().tlora_ckpt_bytes(self.T, self.d_in)):
             raise TloraError("bwd_ckpt: packed has fewer bytes than X's 8-bit form")
-        c_dA, c_dB = _grad_ptr_arrays(len(self.ranks), None if dA is None else [a.data_ptr() if a.numel() else 0 for a in dA],
-                                      None if dB is None else [b.data_ptr() if b.numel() else 0 for b in dB])
+        _holds(packed is None or (packed.is_contiguous() and packed.get_device() == dev),
+               "bwd_ckpt: packed must be contiguous, on the holder's device")
+        elt = t.bfloat16 if self.dtype == "bf16" else t.float32
+        _given("bwd_ckpt", (("dY", dY),), (self.T, self.d_out), elt, dev)
+        _given("bwd_ckpt", (("dX", dX),), (self.T, self.d_in), elt, dev)
+        _holds((dA is None) == (dB is None), "bwd_ckpt: dA and dB come together")
+        for name, grads, width in (("dA", dA, self.d_in), ("dB", dB, self.d_out)):
+            _holds(grads is None or len(grads) == len(self.ranks), f"bwd_ckpt: one gradient per job in {name}")
+            for j, r in enumerate(self.ranks if grads is not None else ()):
+                _given("bwd_ckpt", ((f"{name}[{j}]", grads[j] if r else None),), (width * r,), t.float32, dev)
+        stream = _call_stream(t, dev, "bwd_ckpt")
+        c_dA, c_dB = _grad_ptr_arrays(len(self.ranks), None if dA is None else [_ptr(a) or 0 for a in dA],
+                                      None if dB is None else [_ptr(b) or 0 for b in dB])
         _check(lib().tlora_bwd_ckpt(ctypes.byref(self.prob), _ptr(packed), _ptr(dY), _ptr(dX), c_dA, c_dB,
                                     (TLORA_BWD_REUSE_S if reuse_S else 0) | flags, ctypes.c_void_p(self.ws.data_ptr()),
-                                    ctypes.c_size_t(self.ws_bytes), ctypes.c_void_p(self._stream())), "tlora_bwd_ckpt")
+                                    ctypes.c_size_t(self.ws_bytes), ctypes.c_void_p(stream)), "tlora_bwd_ckpt")
 
     def _nano_ws(self, n_nano: int, granule: int) -> None:
         """Grow the workspace if this partition needs more (the whole batch's covers every partition of it)."""
@@ -834,11 +846,46 @@ def _holds(ok: bool, what: str) -> None:
         raise TloraError(what)
 
 
+def _given(what: str, tensors, shape, dtype, device: int) -> None:
+    """The tensors of a call, (name, tensor or None): dense, of this dtype and device; of shape [n, width] also [.., width] with n rows or
+    more, of shape [n] n numbers or more.  (A tensor costs 0.2 us of a call that may take 5: the usual shape is asked for first.)"""
+    for name, t in tensors:
+        if t is None or (t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.shape == shape):
+            continue
+        n = shape[0] if len(shape) == 1 else shape[0] * shape[1]
+        if not (t.dtype == dtype and t.get_device() == device and t.is_contiguous() and t.numel() >= n
+                and (len(shape) == 1 or (t.dim() and t.size(-1) == shape[1]))):
+            size = " x ".join(str(v) for v in shape)
+            raise TloraError(f"{what}: {name} must be contiguous {dtype}, {size} or more, on the holder's device")
+
+
+def _one_device(what: str, tensors, device: int) -> None:
+    for name, t in tensors:
+        _holds(t is None or t.get_device() == device, f"{what}: {name} is on another device")
+
+
 def _current_stream(torch) -> int:
     """Handle of the current device's current stream.  Calls of a few rows end as fast as the host can make them, and of such a call's
     7.5 us the Stream object that torch.cuda.current_stream() makes took 2.6; torch's own lookup of the handle takes 0.3."""
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+
+
+_device_calls = None
+
+
+def _call_stream(torch, device: int, what: str) -> int:
+    """That handle, for a call whose tensors are on `device`: the library launches on the current one."""
+    global _device_calls
+    if device < 0:
+        raise TloraError(f"{what}: the tensors must be on a GPU")
+    if _device_calls is None:            # (torch's own functions where it has them: no initialisation is left to do for tensors on a GPU)
+        _device_calls = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                         getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cuda.current_stream(d).cuda_stream))
+    current, stream = _device_calls
+    if current() != device:
+        raise TloraError(f"{what}: the tensors are on GPU {device}, which is not the current one")
+    return stream(device)
 
 
 class ResidualNorm:
@@ -851,10 +898,13 @@ class ResidualNorm:
         self.offsets = [int(o) for o in offsets]
         J = len(self.offsets) - 1
         self.J, self.d = J, int(Y.shape[1])
+        self._rows = (self.offsets[-1], self.d)
+        self.device, self.elt = Y.get_device(), torch.bfloat16 if dtype == "bf16" else torch.float32
         self._off = (ctypes.c_int64 * (J + 1))(*self.offsets)
         vectors = {f"gates[{j}]": g for j, g in enumerate(gates or [])}
         tensors = dict(X=X, Y=Y, gamma_pre=gamma_pre, gamma_post=gamma_post, **vectors)
-        _dense(tensors, dict.fromkeys(tensors, torch.bfloat16 if dtype == "bf16" else torch.float32), "ResidualNorm")
+        _dense(tensors, dict.fromkeys(tensors, self.elt), "ResidualNorm")
+        _one_device("ResidualNorm", tensors.items(), self.device)
         for name, t in dict(X=X, Y=Y).items():
             _holds(t is None or (t.dim() == 2 and t.shape[1] == self.d and t.shape[0] >= self.offsets[-1]),
                    f"ResidualNorm: {name} must be [{self.offsets[-1]} or more, {self.d}]")
@@ -865,23 +915,30 @@ class ResidualNorm:
         self._keep = [X, Y, gamma_pre, gamma_post, gates]
         self.prob = tlora_norm_t(TLORA_BF16 if dtype == "bf16" else TLORA_F32, J, self.d, self._off, float(eps), float(res_scale),
                                  _ptr(X), _ptr(Y), _ptr(gamma_post), _ptr(gamma_pre), self._gates)
-        self.ws_bytes = int(lib().tlora_norm_workspace_bytes(ctypes.byref(self.prob)))
+        self._ref = ctypes.byref(self.prob)
+        self.ws_bytes = int(lib().tlora_norm_workspace_bytes(self._ref))
         if self.ws_bytes == 0:
             raise TloraError("tlora_norm_workspace_bytes: invalid problem")
         self.ws = None               # (made by the first bwd: a forward has no use for it)
 
     def _stream(self):
-        return _current_stream(self.torch)
+        return _call_stream(self.torch, self.device, "ResidualNorm")
 
     def fwd(self, H, Xn) -> None:
-        _check(lib().tlora_norm_fwd(ctypes.byref(self.prob), _ptr(H), _ptr(Xn), self._stream()), "tlora_norm_fwd")
+        _given("ResidualNorm.fwd", (("H", H), ("Xn", Xn)), self._rows, self.elt, self.device)
+        _check(lib().tlora_norm_fwd(self._ref, _ptr(H), _ptr(Xn), self._stream()), "tlora_norm_fwd")
 
     def bwd(self, dH, dXn, dX, dY, dgamma_post=None, dgamma_pre=None, dgates=None, flags: int = 0) -> None:
+        _given("ResidualNorm.bwd", (("dH", dH), ("dXn", dXn), ("dX", dX), ("dY", dY)), self._rows, self.elt, self.device)
+        _holds(dgates is None or len(dgates) == self.J, "ResidualNorm.bwd: one gradient (or None) per job in dgates")
+        _given("ResidualNorm.bwd", (("dgamma_post", dgamma_post), ("dgamma_pre", dgamma_pre),
+                                    *((f"dgates[{j}]", t) for j, t in enumerate(dgates or ()))), (self.d,), self.torch.float32, self.device)
+        stream = self._stream()
         if self.ws is None:
             self.ws = self.torch.empty(self.ws_bytes, dtype=self.torch.uint8, device=self._keep[1].device)
         g = None if dgates is None else (ctypes.c_void_p * self.J)(*[_ptr(t) for t in dgates])
-        _check(lib().tlora_norm_bwd(ctypes.byref(self.prob), _ptr(dH), _ptr(dXn), _ptr(dX), _ptr(dY), _ptr(dgamma_post),
-                                    _ptr(dgamma_pre), g, int(flags), self.ws.data_ptr(), self.ws_bytes, self._stream()), "tlora_norm_bwd")
+        _check(lib().tlora_norm_bwd(self._ref, _ptr(dH), _ptr(dXn), _ptr(dX), _ptr(dY), _ptr(dgamma_post),
+                                    _ptr(dgamma_pre), g, int(flags), self.ws.data_ptr(), self.ws_bytes, stream), "tlora_norm_bwd")
 
 
 class LossHead:
@@ -898,6 +955,8 @@ class LossHead:
         _dense(dict(H=H, W=W, targets=targets, weights=weights),
                dict(H=torch.bfloat16, W=torch.bfloat16, targets=torch.int32, weights=torch.float32), "LossHead")
         T, d = self.offsets[-1], int(W.shape[0])
+        self.J, self.T, self.d, self.device = J, T, d, W.get_device()
+        _one_device("LossHead", (("H", H), ("targets", targets), ("weights", weights)), self.device)
         _holds(H is None or (H.dim() == 2 and H.shape[1] == d and H.shape[0] >= T), f"LossHead: H must be [{T} or more, {d}]")
         for name, t in dict(targets=targets, weights=weights).items():
             _holds(t is None or t.numel() >= T, f"LossHead: {name} must have {T} elements or more")
@@ -910,12 +969,19 @@ class LossHead:
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=W.device)
 
     def _tail(self):
-        return self.ws.data_ptr(), self.ws_bytes, _current_stream(self.torch)
+        return self.ws.data_ptr(), self.ws_bytes, _call_stream(self.torch, self.device, "LossHead")
+
+    def _losses(self, what: str, job_loss, *per_token) -> None:
+        _given(what, per_token, (self.T,), self.torch.float32, self.device)
+        _given(what, (("job_loss", job_loss),), (self.J,), self.torch.float32, self.device)
 
     def fwd(self, loss, lse, job_loss) -> None:
+        self._losses("LossHead.fwd", job_loss, ("loss", loss), ("lse", lse))
         _check(lib().tlora_ce_fwd(ctypes.byref(self.prob), _ptr(loss), _ptr(lse), _ptr(job_loss), *self._tail()), "tlora_ce_fwd")
 
     def fwd_bwd(self, loss, lse, job_loss, dH, dloss=None) -> None:
+        self._losses("LossHead.fwd_bwd", job_loss, ("loss", loss), ("lse", lse), ("dloss", dloss))
+        _given("LossHead.fwd_bwd", (("dH", dH),), (self.T, self.d), self.torch.bfloat16, self.device)
         _check(lib().tlora_ce_fwd_bwd(ctypes.byref(self.prob), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(job_loss), _ptr(dH),
                                       *self._tail()), "tlora_ce_fwd_bwd")
 
@@ -932,13 +998,14 @@ class Checkpoint:
         self.packed = torch.empty(n, dtype=torch.uint8, device=device)
 
     def _stream(self):
-        return _current_stream(self.torch)
+        return _call_stream(self.torch, self.packed.get_device(), "Checkpoint")
 
     def _check(self, X) -> None:
         t = self.torch
         _dense(dict(X=X), dict(X=t.bfloat16 if self.code == TLORA_BF16 else t.float32), "Checkpoint")
         if X.numel() != self.T * self.d:
             raise TloraError("Checkpoint: X has another size")
+        _one_device("Checkpoint", (("X", X),), self.packed.get_device())
 
     def pack(self, X) -> None:
         self._check(X)
