@@ -409,7 +409,7 @@ int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float
  * tensor's dtype: |x^ - x| <= s / 2 and that rounding.  A group with a value that is infinite, not a number, or 2^127 or larger comes
  * back as NaN.
  * packed: DEVICE, 256-byte aligned, tlora_ckpt_bytes(T, d): int8 [T, d], then, from the next multiple of 256 bytes on, the scales,
- * bf16 [T, ceil(d / TLORA_CKPT_GROUP)].  d a multiple of 8 and at most TLORA_MAX_FEATURES, 0 <= T <= TLORA_MAX_TOKENS, fewer than 2^30
+ * bf16 [T, ceil(d / TLORA_CKPT_GROUP)].  d a multiple of 8 and at most TLORA_MAX_FEATURES, 0 <= T <= TLORA_MAX_TOKENS, at most 2^30 - 64
  * groups in all (TLORA_EINVAL otherwise); X: DEVICE [T, d] of `dtype`, 16-byte aligned.
  * tlora_bwd_ckpt is tlora_bwd of the problem whose X are the packed values x^: p->X is not read and may be NULL.  With
  * TLORA_BWD_REUSE_S the S_j of the tlora_fwd before it on this workspace are taken (made from the X that the forward had), otherwise

@@ -2418,10 +2418,11 @@ int tlora_ce_fwd_bwd(const tlora_ce_t* p, const float* dloss, float* loss, float
 
 // ---- activations kept in 8 bits ------------------------------------------------------------------------------
 namespace {
+constexpr int64_t kCkptMostGroups = ((int64_t)1 << 30) - 64;     // 64 to a workgroup of 256 threads, less than 2^32 to a launch
 int ckpt_sizes(int64_t tokens, int32_t d) {
   if (tokens < 0 || tokens > TLORA_MAX_TOKENS || d < 8 || d % 8 || d > TLORA_MAX_FEATURES) return TLORA_EINVAL;
   const int64_t groups = (d + TLORA_CKPT_GROUP - 1) / TLORA_CKPT_GROUP;
-  return tokens * groups < (int64_t)1 << 30 ? TLORA_OK : TLORA_EINVAL;        // four threads each, less than 2^32 to a launch
+  return tokens * groups <= kCkptMostGroups ? TLORA_OK : TLORA_EINVAL;
 }
 size_t ckpt_scales_at(int64_t tokens, int32_t d) { return align_up((size_t)tokens * (size_t)d, 256); }
 int ckpt_checks(int32_t dtype, const void* X, int64_t tokens, int32_t d, const void* packed) {

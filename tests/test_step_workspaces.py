@@ -83,3 +83,15 @@ def test_a_holder_keeps_what_its_workspace_held():
     layer.bwd_ckpt_workspace()
     assert layer.ws_bytes == layer.ws.numel() > before.numel()
     assert torch.equal(layer.ws[:before.numel()], before)
+
+
+@pytest.mark.parametrize("behind,groups,tokens", [(-65, 439, 2445881), (-64, 64, 16777215), (-62, 131, 8196502), (-1, 77, 13944699)])
+def test_eight_bits_of_a_full_launch(behind, groups, tokens):
+    # 64 groups to a workgroup: 2^24 - 1 workgroups of 256 threads are the most below 2^32 threads
+    L = tlora.lib()
+    assert groups * tokens == (1 << 30) + behind
+    fits = -(-groups * tokens // 64) * 256 < 1 << 32
+    assert (L.tlora_ckpt_bytes(tokens, 128 * groups) > 0) == fits == (behind <= -64)
+    if not fits:
+        assert L.tlora_ckpt_pack(1, P(0x1000), tokens, 128 * groups, P(WS), None) == -1
+        assert L.tlora_ckpt_unpack(1, P(WS), tokens, 128 * groups, P(0x1000), None) == -1
