@@ -2319,7 +2319,10 @@ int ce_plan(const tlora_ce_t* p, bool grad, CePlan& C) {
     C.off_E_tail = place(2 * n * 32);
     C.off_W_tail = place(2 * d * 32);
   }
-  C.off_part = place(kHeadPartBytes);
+  // (the two products use it in turn; logits of a d_model that is no multiple of a K-step are not cut)
+  const size_t logits_part = p->d_model % kGemmBK ? 0 : head_part_bytes(C.piece, C.col_tiles, p->d_model / kGemmBK);
+  const int grad_steps = (p->vocab + kGemmBK - 1) / kGemmBK, grad_tiles = (p->d_model + kGemmBN - 1) / kGemmBN;
+  C.off_part = place(std::max(logits_part, grad ? head_part_bytes(C.piece, grad_tiles, grad_steps) : 0));
   C.total = w;
   return TLORA_OK;
 }

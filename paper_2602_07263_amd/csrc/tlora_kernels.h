@@ -137,14 +137,21 @@ struct HeadParams {
 };
 constexpr int kHeadMaxSplits = 64;
 constexpr int kHeadShare = 8;            // K-steps
-constexpr size_t kHeadPartBytes = (size_t)512 * kGemmBM * kGemmBN * sizeof(float);   // sums of the shares: at most two rounds of tiles
+// Bytes of the shares' sums of a product of at most max_rows rows, whatever their number turns out to be (head_shape): at most two
+// rounds of tiles, and none of a contraction that is too short to be cut.
+inline size_t head_part_bytes(int64_t max_rows, int tiles_n, int steps) {
+  const int64_t most = steps / kHeadShare < kHeadMaxSplits ? steps / kHeadShare : kHeadMaxSplits;
+  const int64_t tiles = (max_rows + kGemmBM - 1) / kGemmBM * tiles_n, rest = tiles < 255 ? tiles : 255;
+  const int64_t shares = most < 2 ? 0 : rest * most < 512 ? rest * most : 512;
+  return (size_t)shares * kGemmBM * kGemmBN * sizeof(float);
+}
 // Largest logit of a row in a tile up to which exp(z) needs no reference, and from which on sums of it hold their digits.
 __host__ __device__ inline float head_reference(float m) {
   constexpr float kTop = 60.f, kBottom = -40.f;
   return m <= kTop && m >= kBottom ? 0.f : m == -__builtin_huge_valf() ? 0.f : m;
 }
 // E = exp(H.W - ref) as bf16 [max_rows, ld] (null: statistics alone), zero from vocab to the next multiple of 8; stats; target_logit.
-// Tiles that are cut leave their shares in part (kHeadPartBytes), from which launch_head_logits_reduce makes the same.
+// Tiles that are cut leave their shares in part (head_part_bytes), from which launch_head_logits_reduce makes the same.
 void launch_head_logits(const HeadParams& head, const uint16_t* H, const uint16_t* W, uint16_t* E, int d, float* part, hipStream_t st);
 void launch_head_logits_reduce(const HeadParams& head, uint16_t* E, int d, const float* part, hipStream_t st);
 // dH[out_index[r]] = factor[r] * (E[r] . W^T).  The columns from vocab / 32 * 32 on come from E_tail [max_rows padded to 256, 32] and

@@ -95,3 +95,47 @@ def test_eight_bits_of_a_full_launch(behind, groups, tokens):
     if not fits:
         assert L.tlora_ckpt_pack(1, P(0x1000), tokens, 128 * groups, P(WS), None) == -1
         assert L.tlora_ckpt_unpack(1, P(WS), tokens, 128 * groups, P(0x1000), None) == -1
+
+
+def _shares(rows, tiles_n, steps):
+    """Tiles of fp32 sums that a product of `rows` rows leaves: whole rounds of 256 tiles as they are, the rest in shares."""
+    rest = -(-rows // 256) * tiles_n % 256
+    if not rest:
+        return 0
+    extra, most = 32 * min(rows, 256) // 256, min(64, max(steps // 8, 1))
+    s1, s2 = min(256 // rest, most), min(512 // rest, most)
+    cost1 = -(-steps // s1) + extra if s1 > 1 else steps
+    cost2 = 2 * (-(-steps // s2) + extra)
+    n = s2 if cost2 < cost1 and rest * s2 > 256 else s1 if s1 > 1 and cost1 < steps else 1
+    return rest * n if n > 1 else 0
+
+
+def _ce_sizes(T, d, V):
+    ld = (V + 7) // 8 * 8
+    off = (ctypes.c_int64 * 2)(0, T)
+    q = tlora.tlora_ce_t(tlora.TLORA_BF16, 1, d, V, ld, off, P(0x1000), P(0x2000), P(0x3000), None)
+    return [tlora.lib().tlora_ce_workspace_bytes(ctypes.byref(q), g) for g in (0, 1)], ld
+
+
+@pytest.mark.parametrize("d,V", [(64, 9), (64, 1000), (72, 5000), (1024, 600), (512, 50000), (4096, 32000), (8192, 259)])
+def test_the_losses_workspace_holds_the_shares_of_any_number_of_rows(d, V):
+    tile = 256 * 256 * 4
+    last = [0, 0]
+    for T in (1, 61, 256, 257, 1500, 4096, 5000, 20000):
+        sizes, ld = _ce_sizes(T, d, V)
+        for g in (0, 1):
+            piece = min(4096 if g else 16384, -(-T // 256) * 256)
+            logits = max(_shares(r, -(-V // 256), d // 32) for r in range(1, min(piece, T) + 1, 1 if T < 300 else 17)) if d % 32 == 0 else 0
+            grads = max(_shares(r, -(-d // 256), -(-V // 32)) for r in range(1, min(piece, T) + 1, 1 if T < 300 else 17)) if g else 0
+            # beside them a piece's rows, exponentials and statistics
+            others = 2 * piece * d + 8 * piece * -(-V // 256) + (2 * piece * ld if g else 0)
+            assert sizes[g] >= others + tile * max(logits, grads)
+            assert sizes[g] >= last[g]
+        last = sizes
+    assert sizes[1] <= 2 * 16384 * d + 8 * 16384 * -(-V // 256) + 2 * 4096 * ld + 512 * tile + (1 << 20)
+
+
+def test_a_small_loss_has_a_small_workspace():
+    for T, d, V in ((61, 64, 200), (500, 128, 250), (61, 72, 255)):
+        sizes, _ = _ce_sizes(T, d, V)
+        assert max(sizes) < 1 << 20

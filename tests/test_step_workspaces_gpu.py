@@ -1,4 +1,4 @@
-"""The backward from 8 bits on the plain workspace, where that is enough: the bits that a larger one gives, and nothing behind it written."""
+"""Workspaces of just the stated size: the bits that larger ones give, and nothing behind them written."""
 import pytest
 
 from paper_2602_07263_amd import workloads as wk
@@ -62,3 +62,25 @@ def test_a_workspace_that_grows_behind_the_forward_keeps_its_S():
         results.append(dA + dB)
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,d,V", [(5, 64, 200), (61, 4096, 32000), (300, 512, 50000), (700, 8192, 259), (257, 72, 5000), (5000, 256, 3001)])
+def test_the_losses_workspace_is_enough(T, d, V):
+    import torch
+    from paper_2602_07263_amd import tlora
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    rn = lambda *n: torch.randn(*n, device="cuda", generator=g).to(torch.bfloat16)
+    H, W = rn(T, d), rn(d, (V + 7) // 8 * 8) * (2 * d ** -0.5)
+    y = torch.randint(-1, V, (T,), device="cuda", generator=g, dtype=torch.int32)
+    head, results = tlora.LossHead([0, T // 3, T], H, W, V, y), []
+    for guard in (1 << 27, 4096):
+        head.ws = torch.full((head.ws_bytes + guard,), 0xAB, dtype=torch.uint8, device="cuda")
+        out = [torch.full(n, float("nan"), device="cuda") for n in ((T,), (T,), (2,))] + [torch.full_like(H, float("nan"))]
+        print(f"{T} {d} {V} {guard}", flush=True)
+        head.fwd_bwd(*out)
+        torch.cuda.synchronize()
+        assert (head.ws[head.ws_bytes:] == 0xAB).all()
+        results.append(out)
+    for a, b in zip(*results):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
