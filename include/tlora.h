@@ -346,7 +346,9 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
  *     dgate_j = sum_{t of job j} res_scale * D * N
  * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs
  * gamma_post (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or added to with TLORA_BWD_ACCUMULATE (the only flag);
- * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap no inputs.
+ * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap neither inputs nor
+ * one another (an entry of dgates that is there twice is refused, TLORA_EINVAL; gates may be shared, their gradients then added up by the
+ * caller).
  * mean(V^2) + eps of a row is to lie between 2^-80 and 2^80, and results and their terms are to be ordinary fp32 numbers; outside (a row of
  * zeros with eps 0, say) that row, and the sums it enters, may be infinite, not a number or wrong.
  * tlora_norm_fwd needs no workspace.  tlora_norm_bwd's: 256-byte aligned, tlora_norm_workspace_bytes.  Neither call allocates,
@@ -383,7 +385,7 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  * the largest term, is mostly made good by the row's factor, which moves the others by half a step at most); logits are not kept.  Logits, sums and
  * statistics are fp32.  loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
  * bf16 only (TLORA_EDTYPE otherwise); d_model a multiple of 8; vocab >= 1, of any size; ld_w a multiple of 8, vocab <= ld_w <=
- * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned; outputs overlap no inputs.
+ * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned; outputs overlap neither inputs nor one another.
  * The workspace depends on num_jobs, T, d_model, vocab, ld_w and with_grad (0: tlora_ce_fwd, else either call), and never
  * falls when tokens are added.  Neither call allocates, copies or synchronises, so both may be captured into a graph. */
 typedef struct {

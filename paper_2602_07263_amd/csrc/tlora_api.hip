@@ -2230,12 +2230,15 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
   if (misaligned16(dH) || misaligned16(dXn) || misaligned16(dX) || misaligned16(dY) || misaligned16(dgamma_post) ||
       misaligned16(dgamma_pre))
     return TLORA_EALIGN;
-  bool want_gates = false;
+  std::vector<const float*> wanted;
   if (dgates)
     for (int j = 0; j < p->num_jobs; ++j) {
-      want_gates = want_gates || dgates[j];
       if (misaligned16(dgates[j])) return TLORA_EALIGN;
+      if (dgates[j]) wanted.push_back(dgates[j]);
     }
+  const bool want_gates = !wanted.empty();
+  std::sort(wanted.begin(), wanted.end());             // (every job's is written by workgroups of its own)
+  if (std::adjacent_find(wanted.begin(), wanted.end()) != wanted.end()) return TLORA_EINVAL;
   if (bad_ws(workspace, ws_bytes, N.total)) return TLORA_EWORKSPACE;
   rc = check_arch();
   if (rc != TLORA_OK) return rc;

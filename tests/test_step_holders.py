@@ -75,3 +75,18 @@ def test_inputs_on_several_devices():
         tlora._one_device("holder", (("X", None), ("Y", y)), 0)
     with pytest.raises(tlora.TloraError, match="must be on a GPU"):
         tlora._call_stream(torch, -1, "holder")
+
+
+def test_two_jobs_with_one_gradient_of_a_gate_are_refused():
+    import ctypes
+    P, L = ctypes.c_void_p, tlora.lib()
+    off = (ctypes.c_int64 * 4)(0, 1, 2, 4)
+    gates = (P * 3)(0x5000, 0x5000, None)                # (a gate that two jobs share is read alone)
+    q = tlora.tlora_norm_t(tlora.TLORA_BF16, 3, 64, off, 1e-5, 1.0, None, P(0x2000), None, None, gates)
+    n = L.tlora_norm_workspace_bytes(ctypes.byref(q))
+    # (the size of the workspace is looked at last: a call whose gradients are apart is refused for it)
+    call = lambda dg, ws: L.tlora_norm_bwd(ctypes.byref(q), P(0x8000), None, P(0xA000), None, None, None, (P * 3)(*dg), 0, P(0x100000), ws, None)
+    for dg in ((0xE000, 0xE000, None), (0xE000, 0xF000, 0xE000), (None, 0xF000, 0xF000)):
+        assert call(dg, n) == -1
+    for dg in ((0xE000, 0xF000, 0xE100), (None, 0xF000, None), (None, None, None)):
+        assert call(dg, n - 1) == -4
