@@ -344,11 +344,11 @@ int tlora_layer_bwd(const tlora_layer_t* p, const void* dOut, void* dX, void* co
  *     D = dH + d norm(H; gamma_pre)^T dXn;   dX = D;   dY = d norm(Y; gamma_post)^T (res_scale * gate_j * D)
  *     dgamma_pre = sum_t dXn * H rstd_H;   dgamma_post = sum_t res_scale * gate_j * D * Y rstd_Y;
  *     dgate_j = sum_{t of job j} res_scale * D * N
- * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs
- * gamma_post (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or added to with TLORA_BWD_ACCUMULATE (the only flag);
- * those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a multiple of 8; outputs overlap neither inputs nor
- * one another (an entry of dgates that is there twice is refused, TLORA_EINVAL; gates may be shared, their gradients then added up by the
- * caller).
+ * dX, dY, dgamma_*, dgates and entries of dgates may be NULL (not wanted).  dgamma_post (dgamma_pre, dXn) needs gamma_post
+ * (gamma_pre), dgates needs gates, and Xn gamma_pre (TLORA_ENULL otherwise).  dgamma_* and dgates are fp32 [d_model], overwritten, or
+ * added to with TLORA_BWD_ACCUMULATE (the only flag); those of a job without tokens are zero.  Tensors are 16-byte aligned, d_model a
+ * multiple of 8; outputs overlap neither inputs nor one another.  (Jobs may share a gate; an entry of dgates that is there twice is
+ * refused, TLORA_EINVAL: the caller adds such gradients up.)
  * mean(V^2) + eps of a row is to lie between 2^-80 and 2^80, and results and their terms are to be ordinary fp32 numbers; outside (a row of
  * zeros with eps 0, say) that row, and the sums it enters, may be infinite, not a number or wrong.
  * tlora_norm_fwd needs no workspace.  tlora_norm_bwd's: 256-byte aligned, tlora_norm_workspace_bytes.  Neither call allocates,
@@ -380,12 +380,15 @@ int tlora_norm_bwd(const tlora_norm_t* p, const void* dH, const void* dXn, void*
  * weights sum to zero has job_loss 0, of which there is no gradient.  Other weights than 0 have no say in a gradient made from dloss.
  * tlora_ce_fwd_bwd also makes  dH_t = g_t (softmax(z_t) - onehot(y_t)) . W^T  with g_t = dloss[t] (DEVICE fp32 [T]) or, with
  * dloss NULL, of L = sum_j job_loss_j.  W is frozen: no gradient.
- * Pieces of at most 4096 tokens are taken one after the other, and of a piece the exponentials exp(z) are kept as bf16 between the two
- * products (half a step of a bf16 number off, as the probabilities of tlora_attention_*; the rounding of softmax - 1 at the target,
- * the largest term, is mostly made good by the row's factor, which moves the others by half a step at most); logits are not kept.  Logits, sums and
- * statistics are fp32.  loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
+ * Pieces of at most 4096 tokens (16384 without a gradient) are taken one after the other.  With a gradient the exponentials exp(z) of a
+ * piece are kept as bf16 between the two products (half a step of a bf16 number off, as the probabilities of tlora_attention_*; the
+ * rounding of softmax - 1 at the target, the largest term, is mostly made good by the row's factor, which moves the others by half a
+ * step at most).  Logits leave the registers only as fp32 shares of tiles whose contraction is cut.  Logits, sums and statistics are
+ * fp32; the gradient sums products of W with exponentials of up to e^60, so that elements of W are to be below 2^40 in magnitude.
+ * loss, lse (DEVICE fp32 [T]) and job_loss (DEVICE fp32 [J]) may be NULL (not wanted).
  * bf16 only (TLORA_EDTYPE otherwise); d_model a multiple of 8; vocab >= 1, of any size; ld_w a multiple of 8, vocab <= ld_w <=
- * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned; outputs overlap neither inputs nor one another.
+ * TLORA_MAX_FEATURES, all d_model * ld_w elements readable (what lies behind column vocab has no effect); H, W, dH 16-byte aligned;
+ * outputs overlap neither inputs nor one another.
  * The workspace depends on num_jobs, T, d_model, vocab, ld_w and with_grad (0: tlora_ce_fwd, else either call), and never
  * falls when tokens are added.  Neither call allocates, copies or synchronises, so both may be captured into a graph. */
 typedef struct {

@@ -2117,7 +2117,7 @@ int norm_plan(const tlora_norm_t* p, NormPlan& N) {
   // Rows of a unit: as few as let all units run at a time (a few more of them than fit, as whole units of every job make them, take
   // as long again: 516 units of 62 rows 405 us, 504 of 64 316).  While there are few rows a short chain of them counts against the
   // partial sums of many units: with 1, 2, 4 rows to a unit 128 rows of 4096 features take 11.3, 11.6, 13.2 us, 300 rows 18.8, 13.7,
-  // 15.0, and 1024 rows 22.3, 22.1, 18.6.
+  // 15.0, and 1024 rows 22.3, 22.1, 18.6.  (bf16, all sums; other widths and fp32 have the same rule without a sweep of their own.)
   const int64_t fit = norm_resident_units(p->dtype == TLORA_BF16, p->d_model);
   auto count = [&]() {
     auto units = [&](int64_t rows) { return (rows + N.unit_rows - 1) / N.unit_rows; };

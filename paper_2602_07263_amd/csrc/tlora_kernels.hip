@@ -574,7 +574,7 @@ constexpr int waitcnt_vm_lgkm0(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 
 // ---------------------------------------------------------------------------------------------------
 // Q8: the activations are 8-bit codes with a scale per row and 128 values (activations kept in 8 bits): half the bytes of X, which
 // become bf16 on the way to the matrix instruction, as the unpacked tensor would have them.  The scales of a unit's rows are put
-// into LDS first (kShrinkScales of them at most).  31744 x 4096, ranks 4 to 128: 59 us, as long as from bf16 (a step's chain of barrier,
+// into LDS first (kShrinkScales of them at most).  31744 x 4096, ranks 4 to 128: 62 us, as long as from bf16 (a step's chain of barrier,
 // reads, conversion and products sets the pace), without the 65 us of unpacking before it.
 // PCOLS: rank columns staged per step.  A unit whose job has at most 32 (64) padded rank columns stages such an
 // adapter tile and spends the LDS it saves on more stages: the kernel is bound by the bytes of X in flight.
@@ -1027,8 +1027,8 @@ struct GemmParams {
 
 // What a tile of logits leaves of itself.  A lane holds tokens 16 i + l % 16 of its wave's 128 rows and features 4 (l / 16) .. + 3 of
 // each of the wave's four blocks of 16 columns.  The row's exponentials are taken relative to 0 where its largest logit in the tile
-// lies within kHeadPlain, so that the tiles of a row agree on the reference and the gradient's product can add them up as they are;
-// a bf16 exponential has the same 8 significant bits at any size.  Outside of that the reference is the largest logit itself.
+// lies within head_reference's bounds, so that the tiles of a row agree on the reference and the gradient's product can add them up as
+// they are; a bf16 exponential has the same 8 significant bits at any size.  Outside of that the reference is the largest logit itself.
 // scratch: 2 x 4 x 256 floats.
 __device__ __forceinline__ void head_softmax_tile(const HeadParams& h, f32x4 (&acc)[4][8], float* scratch, int row0, int rows_valid, int tn,
                                                   int wm, int wn, int lane, int tid) {
@@ -1965,7 +1965,7 @@ __device__ __forceinline__ bf16x8 frag_tr_u(const uint8_t* plane, int pitch, int
 // Q8: V are 8-bit codes with a scale per row and 128 columns (activations kept in 8 bits).  Half the bytes of V come from memory; a
 // fragment is one transposing read of bytes and becomes bf16 on the way to the matrix instruction, as the unpacked tensor would
 // have it.  The scales of a unit's tokens for its two groups of columns are put into LDS first.  7680 tokens of four jobs, 4096 ->
-// 4096, S kept: unpacking 19 us and dA / dB 27 us, now 36; a call of 31744 tokens, 4096 -> 12288, without dX 484 us, now 429.  What is
+// 4096, S kept: unpacking 19 us and dA / dB 27 us, now 37 to 39; a call of 31744 tokens, 4096 -> 12288, without dX 484 us, now 429.  What is
 // left above half of the bf16 time is the conversion: about 3 vector operations per value, in each of the two waves that read it.
 template <bool ONE, bool Q8 = false>
 struct GradShape {

@@ -611,7 +611,7 @@ __device__ __forceinline__ float norm_dot(float dHw, float uw, float hw, float r
 // [unit][3][d] (dgamma_post, dgamma_pre, dgate; those that are wanted).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
 // for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
 // what the second sums give (norm_D), so the last sum is put together from three that need rstd_Y alone (norm_dot); and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
-// barrier.  31744 x 4096 bf16 with all sums 320 us (4.9 TB/s).
+// barrier.  31744 x 4096 bf16 with all sums 320 to 324 us (4.8 TB/s).
 // BOTH: dX and dY are wanted.  Every lane then stores without a condition -- those behind the row's end its last features once more,
 // the same values -- since behind a store that may not have been issued the compiler waits for all those that may.
 template <bool BF, bool SUMS, bool BOTH>
