@@ -36,9 +36,9 @@ __device__ __forceinline__ double block_sum_1024(double x, double* red) {
 // ---------------------------------------------------------------------------------------------------
 // Cross entropy.  Workgroup 0 lists the tokens that have a loss, in token order; workgroup 1 + j sums job j's weights and notes
 // what each of its tokens' losses counts for (dloss, or weight / sum; nothing at weight 0).  Tokens without a loss get zeros.  Of the
-// workgroups behind those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the batch is one
-// piece moves the others' rows of H to their places, for which it counts the list up to its tokens itself (16 KB of targets at
-// most, from the L2; a launch of its own that reads the list would cost more); the last copy the end of W.
+// workgroups behind those, each of the first has 16 tokens, a wave per row: it clears the rows of dH without a loss, and where the
+// batch is one piece moves the others' rows of H to their places, for which it counts the list up to its tokens itself (16 KB of
+// targets at most, from the L2; a launch of its own that reads the list would cost more); the last copy the end of W.
 // ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ bool ce_live(int y, int vocab) { return (unsigned)y < (unsigned)vocab; }
 
@@ -316,9 +316,9 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(HeadParams h, CeTokens c
     if (lse) lse[t] = l;
   }
   if (!GRAD) return;
-  // (one row has one share: all lanes agree.  With rho = l the factor is the share itself)
+  // (one row has one share: all lanes agree.  With rho = l the factor is the share itself; 1 + absorb is 1 to within 2^-8)
   const float g = c.share[t], at_zero = fabsf(g) * expf(-l);
-  const float rho = l >= -20.f && l <= 60.f && (g == 0.f || (at_zero >= 0x1p-100f && at_zero <= 0x1p100f)) ? 0.f : l;
+  const float rho = l >= -20.f && l <= 60.f && (g == 0.f || (at_zero >= 0x1p-125f && at_zero <= 0x1p127f)) ? 0.f : l;
   uint16_t* const row = E + (int64_t)r * h.ld;
   const int n8 = (h.vocab + 7) & ~7;
   if (!plain || rho != 0.f)
@@ -610,8 +610,9 @@ __device__ __forceinline__ float norm_dot(float dHw, float uw, float hw, float r
 // Backward of a unit's rows, one after the other; with SUMS the unit's column sums stay in registers and leave as partial
 // [unit][3][d] (dgamma_post, dgamma_pre, dgate; those that are wanted).  What holds a row up are the sums across the workgroup that follow one another: of Y^2
 // for rstd_Y, with it of H^2 and dXn gamma_pre H for D, with that of D' = res_scale gate gamma_post D and Y for dY.  D is linear in
-// what the second sums give (norm_D), so the last sum is put together from three that need rstd_Y alone (norm_dot); and Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one
-// barrier.  31744 x 4096 bf16 with all sums 320 to 324 us (4.8 TB/s).
+// what the second sums give (norm_D), so the last sum is put together from three that need rstd_Y alone (norm_dot); and
+// Y^2 is summed for the row after, whose Y is loaded a row earlier than the rest.  So a row has one round of sums and one barrier.
+// 31744 x 4096 bf16 with all sums 320 to 324 us (4.8 TB/s).
 // BOTH: dX and dY are wanted.  Every lane then stores without a condition -- those behind the row's end its last features once more,
 // the same values -- since behind a store that may not have been issued the compiler waits for all those that may.
 template <bool BF, bool SUMS, bool BOTH>

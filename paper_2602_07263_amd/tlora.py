@@ -551,7 +551,8 @@ class LayerProblem:
 
     def bwd_ckpt_workspace(self, reuse_S: bool = False) -> None:
         """Grow the workspace to what bwd_ckpt needs, with what a fwd has left in it (S_j, the packed adapters).  A graph captured before
-        still has the address of the old one: capture afterwards.  reuse_S: for calls with reuse_S alone, which of bf16 values with d_in a multiple of 16 need no more than fwd and bwd."""
+        still has the address of the old one: capture afterwards.  reuse_S: for calls with reuse_S alone, which of bf16 values with d_in
+        a multiple of 16 need no more than fwd and bwd."""
         need = int(lib().tlora_ckpt_workspace_bytes(ctypes.byref(self.prob)))
         if need == 0:
             raise TloraError("tlora_ckpt_workspace_bytes: invalid problem")
@@ -875,7 +876,7 @@ _device_calls = None
 
 
 def _call_stream(torch, device: int, what: str) -> int:
-    """That handle, for a call whose tensors are on `device`: the library launches on the current one."""
+    """Handle of the current stream for a call whose tensors are on `device`: the library launches on the current device."""
     global _device_calls
     if device < 0:
         raise TloraError(f"{what}: the tensors must be on a GPU")
