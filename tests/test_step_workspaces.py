@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 from paper_2602_07263_amd import tlora
+from paper_2602_07263_amd import workloads as wk
 
 P = ctypes.c_void_p
 WS = 0x100000
@@ -28,7 +29,7 @@ def _rc(q, n, flags=0, grads=True):
     return tlora.lib().tlora_bwd_ckpt(ctypes.byref(q[0]), P(WS + 16), P(0x5000), P(0x8000), g, g, flags, P(WS), n, None)
 
 
-BATCH_8B = ([5120, 512, 2048, 3584, 3072, 6144, 5120, 6144], [4, 8, 8, 16, 32, 32, 64, 128])
+BATCH_8B = [[int(v) for v in x] for x in (wk.config(2).tokens, wk.config(2).ranks)]      # the benchmark's eight jobs, 31744 tokens
 
 
 def test_a_kept_S_needs_no_room_for_the_values():
